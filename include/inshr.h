@@ -18,6 +18,8 @@
  * inshr_quantize_sketch is the Quantizer with the paper's own bins (log-space sketch, Algorithm 1,
  * and weighted K-Means on its buckets, Algorithms 2 and 3), inshr_search_sketch the search for the
  * fewest such bins that keep the error within eps (Sec. 5, over the number of bins).
+ * Beside the decoder stand the operators that run a layer from its compressed form (inshr_linear, and its
+ * gradients) and compare answers with those of the original checkpoint (inshr_top_logits, inshr_distill).
  *
  * Conventions
  *   - Every function returns 0 on success or a negative INSHR_E_* code; nothing aborts or throws.
@@ -26,8 +28,9 @@
  *     ordinary host memory.  The caller allocates and owns every buffer; the library never frees
  *     caller memory and keeps no caller pointer after a call returns.
  *   - All work is enqueued on the context's stream.  inshr_search and inshr_quantize return
- *     after that work has completed (they read small results back); inshr_delta returns after
- *     enqueueing, use inshr_sync before reading its outputs on the host.
+ *     after that work has completed (they read small results back); inshr_delta, inshr_linear,
+ *     inshr_top_logits, inshr_distill and the gradients return after enqueueing, use inshr_sync
+ *     before reading their outputs on the host.
  *   - Calls on one context must not overlap in time (the context owns scratch memory).
  *   - Order comparisons use integer images of the floats: -0.0 counts as +0.0, denormals are
  *     ordinary values, NaN / Inf are rejected with INSHR_E_NONFINITE.
@@ -366,6 +369,121 @@ int inshr_search_sketch_grid(inshr_ctx *ctx, const inshr_tensor *tensors, const 
                              uint32_t n_pairs, const inshr_sketch_params *params, double eps,
                              inshr_quantized *out, uint32_t *best_pair, inshr_sketch_choice *choice,
                              inshr_sketch_choice *table, uint32_t n_tensors);
+
+/* ---- answers of a compressed checkpoint (Sec. 5: the quality a configuration is judged by) ----- */
+
+/* Elements of activations and logits. */
+#define INSHR_F32 0u
+#define INSHR_BF16 1u
+#define INSHR_F16 2u
+
+/* Activations: none; max(a, 0); a Phi(a); a / (1 + exp(-2 u)) with u = sqrt(2 / pi) (a + 0.044715 a^3)
+ * (the tanh form of the previous); a / (1 + exp(-a)). */
+#define INSHR_ACT_NONE 0u
+#define INSHR_ACT_RELU 1u
+#define INSHR_ACT_GELU 2u
+#define INSHR_ACT_GELU_TANH 3u
+#define INSHR_ACT_SILU 4u
+
+typedef struct {
+    inshr_dequant_in weight; /* as inshr_quantize left it; weight.n == n_out * n_in                   */
+    uint32_t n_out, n_in;    /* 1 <= n_out, n_in <= 2^30                                               */
+    uint32_t in_out;         /* 0: the weight is stored [n_out][n_in]; nonzero: [n_in][n_out]          */
+    uint32_t type;           /* INSHR_F32 ...: elements of all activations of a call                   */
+    uint32_t activation;     /* INSHR_ACT_NONE ...                                                     */
+    uint32_t reserved;       /* 0 */
+    const float *bias;       /* device [n_out], or NULL                                                */
+} inshr_layer;
+
+/* A matrix in device memory: element (r, c) at data[r * stride + c], aligned to its elements.  Rows of
+ * inputs may overlap (stride 0 repeats a row); rows of outputs may not.  data == NULL: not given, or not
+ * wanted, where a call allows that. */
+typedef struct {
+    void *data;
+    uint64_t stride; /* elements */
+} inshr_matrix;
+
+/* y = act(x W^T + bias) + residual on `rows` rows (0 .. 2^22; 0 does nothing), W the decoded weight:
+ * +0.0 for symbol 0, the protected values at their indices, codebook[s - 2] for symbol s >= 2.
+ *   x         [rows][n_in]
+ *   residual  [rows][n_out] or NULL; may be y itself (same address and stride)
+ *   y         [rows][n_out]
+ *   pre       [rows][n_out] or NULL: receives x W^T + bias, which inshr_linear_grad wants
+ * y and pre share no memory with each other or with x.
+ * Sums are held in fp32; a result is rounded once, `pre` on its own.  The factors are fp16 numbers scaled
+ * by powers of two (one per row of x, one for the weight), in two parts each for fp32 results, one and two
+ * for fp16, one each for bfloat16: what that takes from a product is 2^-22, 2^-22 and 2^-11 of it, or 2^-40
+ * of (largest of the row) * (largest of the weight) where that is more.  Infinities and NaN in a row of x
+ * make that row's results infinite or NaN.  The call returns after enqueueing, allocates nothing and may be
+ * captured into a graph; overlapping calls take workspaces of their own.  workspace: device, 256-byte
+ * aligned, inshr_linear_bound() bytes (NULL when that is 0).
+ * The codes are taken as they are (inshr_dequantize checks them): a symbol above K + 1 makes the results
+ * that it enters NaN, listed indices outside the weight are left out, and with a list that is not the
+ * stream's ascending one the results are undefined.
+ * INSHR_E_ARG: a NULL or misaligned pointer, an unknown type or activation, dimensions out of range,
+ * weight.n != n_out * n_in, an output stride below its columns; INSHR_E_CONFIG: the codes' bits / bins;
+ * INSHR_E_CAPACITY: workspace_bytes too small. */
+int inshr_linear_bound(const inshr_layer *layer, uint64_t rows, uint64_t *workspace_bytes);
+int inshr_linear(inshr_ctx *ctx, const inshr_layer *layer, inshr_matrix x, inshr_matrix residual, inshr_matrix y,
+                 inshr_matrix pre, uint64_t rows, void *workspace, uint64_t workspace_bytes);
+
+/* The gradients of inshr_linear for dy [rows][n_out], the gradient of y (and of the residual): with
+ * d = dy * act'(pre),
+ *   dx     [rows][n_in]  d W                                      or NULL
+ *   dw     device fp32, in the layout of the weight: d^T x         or NULL; what inshr_quantize_sens takes
+ *   dbias  device fp32 [n_out]: the sum of d over the rows         or NULL
+ * x is needed for dw, pre (as inshr_linear left it) for every activation but INSHR_ACT_NONE.  The weight
+ * counts as its decoded values: dw is the gradient of each of them, pruned and protected ones included.
+ * rows == 0 sets dw and dbias to zero.  The sums are taken in the same order in every call.  dx and dw do not share
+ * memory with the inputs.  Everything else as inshr_linear; at least one result is wanted.  The bound is
+ * for the results named: want_dx, want_dw. */
+int inshr_linear_grad_bound(const inshr_layer *layer, uint64_t rows, uint32_t want_dx,
+                            uint32_t want_dw, uint64_t *workspace_bytes);
+int inshr_linear_grad(inshr_ctx *ctx, const inshr_layer *layer, inshr_matrix x, inshr_matrix dy, inshr_matrix pre,
+                      inshr_matrix dx, float *dw, float *dbias, uint64_t rows, void *workspace,
+                      uint64_t workspace_bytes);
+
+#define INSHR_MAX_VOCAB (1u << 18)
+#define INSHR_MAX_LISTED 256u
+
+/* The k largest logits of every row, k <= INSHR_MAX_LISTED, k <= n_vocab <= INSHR_MAX_VOCAB, rows 0 .. 2^22:
+ *   index  device int32 [rows][k], by falling value, equal ones by rising index (-0.0 equals +0.0, NaN is above all)
+ *   value  device fp32 [rows][k], the logits
+ *   tail   device fp32 [rows] or NULL: log of the sum of exp(logit / temperature) over the logits that are
+ *          not listed; -inf when these are all -inf or there are none, NaN for a row with NaN or +inf.
+ * temperature > 0, finite.  Returns after enqueueing, allocates nothing and may be captured. */
+int inshr_top_logits(inshr_ctx *ctx, inshr_matrix logits, uint32_t type, uint64_t rows, uint32_t n_vocab, uint32_t k,
+                     float temperature, int32_t *index, float *value, float *tail);
+
+/* A student's logits and what a teacher says of them (inshr_top_logits of the original checkpoint). */
+typedef struct {
+    inshr_matrix logits; /* [rows][n_vocab] of `type`                                                  */
+    const int32_t *index; /* device [rows][k]: places outside 0 .. n_vocab - 1 are empty, and so is one */
+                          /* whose index stands earlier in the row                                      */
+    const float *value;   /* device [rows][k]: the teacher's logits at these                            */
+    const float *tail;    /* device [rows], or NULL: the teacher has nothing but the listed logits      */
+    uint64_t rows;        /* 0 .. 2^22 */
+    uint32_t n_vocab, k, type;
+    float temperature;
+} inshr_distill_in;
+
+/* Distillation from a teacher's top logits.  Per row, with t the listed values / temperature and u the
+ * student's logits / temperature: P = softmax over the listed t and the tail, q = softmax(u), q_rest its sum
+ * over what is not listed;
+ *   loss = sum_listed P (log P - log q) + P_tail (log P_tail - log q_rest)
+ * (without a tail P_tail = 0 and the last term is not there).  A row without a listed entry, whose listed
+ * values and tail are all -inf, or whose logits are all -inf, has loss 0 and gradient 0.  A loss is +inf
+ * where q is 0 and P is not; NaN or +inf in a row makes its loss and gradient NaN.
+ *   loss   device fp32 [rows]
+ *   saved  device fp64 [rows][INSHR_DISTILL_SAVED] for inshr_distill_grad, or NULL
+ * inshr_distill_grad: d loss / d logit = (q_v - P_v) / temperature for a listed v, q_v (1 - P_tail / q_rest) /
+ * temperature for the others (which is their share of q_rest times q_rest - P_tail, and so also where q_rest vanishes), times grad_loss (device fp32 [rows], NULL: 1), into grad [rows][n_vocab] of
+ * `type`, which may be the logits themselves (same address and stride).  saved is inshr_distill's for the same arguments.
+ * Both return after enqueueing, allocate nothing and may be captured. */
+#define INSHR_DISTILL_SAVED 4
+int inshr_distill(inshr_ctx *ctx, const inshr_distill_in *in, float *loss, double *saved);
+int inshr_distill_grad(inshr_ctx *ctx, const inshr_distill_in *in, const double *saved, const float *grad_loss,
+                       inshr_matrix grad);
 
 /* ---- entropy stage of the delta (host memory only, outside the timed path) ------------------- */
 

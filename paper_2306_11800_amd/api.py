@@ -22,6 +22,8 @@ EXPORTS = ["inshr_create", "inshr_destroy", "inshr_strerror", "inshr_last_device
            "inshr_quantize_sketch", "inshr_search_sketch", "inshr_sketch_buckets",
            "inshr_delta_bound", "inshr_delta", "inshr_delta_static", "inshr_guided_search", "inshr_neighbourhood_search", "inshr_dequantize", "inshr_reconstruct",
            "inshr_entropy_encode", "inshr_entropy_decode",
+           "inshr_linear_bound", "inshr_linear", "inshr_linear_grad_bound", "inshr_linear_grad",
+           "inshr_top_logits", "inshr_distill", "inshr_distill_grad",
            "inshr_profile", "inshr_profile_read"]
 
 INSHR_REUSE_SEARCH = 1
@@ -97,6 +99,21 @@ class CDequantIn(C.Structure):
     _fields_ = [("packed", C.c_void_p), ("codebook", C.c_void_p), ("outlier_idx", C.c_void_p),
                 ("outlier_val", C.c_void_p), ("n_outlier", C.c_uint64), ("n", C.c_uint64),
                 ("bits", C.c_uint8), ("protected_bf16", C.c_uint8), ("bins", C.c_uint16)]
+
+
+class CLayer(C.Structure):
+    _fields_ = [("weight", CDequantIn), ("n_out", C.c_uint32), ("n_in", C.c_uint32), ("in_out", C.c_uint32),
+                ("type", C.c_uint32), ("activation", C.c_uint32), ("reserved", C.c_uint32), ("bias", C.c_void_p)]
+
+
+class CMatrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_uint64)]
+
+
+class CDistillIn(C.Structure):
+    _fields_ = [("logits", CMatrix), ("index", C.c_void_p), ("value", C.c_void_p), ("tail", C.c_void_p),
+                ("rows", C.c_uint64), ("n_vocab", C.c_uint32), ("k", C.c_uint32), ("type", C.c_uint32),
+                ("temperature", C.c_float)]
 
 
 class CEntropyStats(C.Structure):
@@ -177,6 +194,17 @@ def load_library() -> C.CDLL:
                                          C.POINTER(CEntropyStats)]
     lib.inshr_entropy_decode.argtypes = [C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint32,
                                          C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.inshr_linear_bound.argtypes = [C.POINTER(CLayer), C.c_uint64, C.POINTER(C.c_uint64)]
+    lib.inshr_linear.argtypes = [C.c_void_p, C.POINTER(CLayer), CMatrix, CMatrix, CMatrix, CMatrix, C.c_uint64,
+                                 C.c_void_p, C.c_uint64]
+    lib.inshr_linear_grad_bound.argtypes = [C.POINTER(CLayer), C.c_uint64, C.c_uint32, C.c_uint32,
+                                            C.POINTER(C.c_uint64)]
+    lib.inshr_linear_grad.argtypes = [C.c_void_p, C.POINTER(CLayer), CMatrix, CMatrix, CMatrix, CMatrix, C.c_void_p,
+                                      C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64]
+    lib.inshr_top_logits.argtypes = [C.c_void_p, CMatrix, C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32, C.c_float,
+                                     C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.inshr_distill.argtypes = [C.c_void_p, C.POINTER(CDistillIn), C.c_void_p, C.c_void_p]
+    lib.inshr_distill_grad.argtypes = [C.c_void_p, C.POINTER(CDistillIn), C.c_void_p, C.c_void_p, CMatrix]
     lib.inshr_profile.argtypes = [C.c_void_p, C.c_int]
     lib.inshr_profile_read.argtypes = [C.c_void_p, C.POINTER(CKernelTime), C.c_uint32,
                                        C.POINTER(C.c_uint32)]
@@ -280,6 +308,73 @@ class Delta:
         self._K = K
 
 
+# -- answers of a compressed checkpoint -------------------------------------------------------------
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_NO_MATRIX = CMatrix(None, 0)
+DISTILL_SAVED = 4  # doubles per row that inshr_distill leaves for inshr_distill_grad
+
+
+class QuantizedLayer:
+    """A linear layer whose weight stays in its compressed form (inshr_layer).  q: what quantize returned for the
+    weight, row-major [n_out][n_in], or [n_in][n_out] with in_out (GPT-2's layout).  bias: float32 [n_out] or None.
+    activation: none, relu, gelu, gelu_tanh or silu.  The buffers of q are read by every call: when q is quantized
+    again, the layer follows after refresh()."""
+    __slots__ = ("q", "n_out", "n_in", "in_out", "bias", "activation", "device", "_c", "_space")
+
+    def __init__(self, q: Quantized, n_out: int, n_in: int, in_out: bool = False, bias: Optional[torch.Tensor] = None,
+                 activation: str = "none"):
+        if activation not in _ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}")
+        if n_out < 1 or n_in < 1 or q.n != n_out * n_in:
+            raise ValueError("the weight does not have n_out * n_in values")
+        self.device = q._bufs[0].device
+        if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != (n_out,) or not bias.is_contiguous()
+                                 or bias.device != self.device):
+            raise ValueError("bias must be a contiguous float32 tensor [n_out] on the weight's device")
+        self.q, self.n_out, self.n_in, self.in_out = q, int(n_out), int(n_in), bool(in_out)
+        self.bias, self.activation = bias, activation
+        self.refresh()
+
+    def refresh(self):
+        """Takes up what q holds now (its buffers, number of bins and protected list)."""
+        q = self.q
+        packed, codebook, _, idx, val = q._ptrs
+        w = CDequantIn(packed, codebook, idx, val, q.n_outlier, q.n, 0, 1 if q.bf16 else 0, q.K)
+        bias = None if self.bias is None else self.bias.data_ptr()
+        self._c = [CLayer(w, self.n_out, self.n_in, self.in_out, t, _ACTIVATIONS[self.activation], 0, bias)
+                   for t in range(len(_TYPES))]
+        self._space = {}  # (call, rows, type) -> workspace bytes
+
+
+@dataclass
+class TopLogits:
+    """A teacher's largest logits: index int32 [rows, k], value float32 [rows, k], tail float32 [rows] (the log of
+    the others' sum at this temperature) or None."""
+    index: torch.Tensor
+    value: torch.Tensor
+    tail: Optional[torch.Tensor]
+    temperature: float = 1.0
+
+
+def _matrix(t: Optional[torch.Tensor], rows, cols, dtype, device, name):
+    """The C matrix of a 2-D tensor with elements of a row side by side."""
+    if t is None:
+        return _NO_MATRIX
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a {dtype} tensor [{rows}, {cols}] on {device} with rows of adjacent elements")
+    # (torch leaves the stride of a single row open, and an output needs one)
+    return CMatrix(t.data_ptr(), t.stride(0) if rows > 1 else cols)
+
+
+def _vector(t: Optional[torch.Tensor], shape, dtype, device, name):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}")
+    return t.data_ptr()
+
+
 def _tensor_array(tensors: Sequence[torch.Tensor]):
     if isinstance(tensors, TensorBatch):
         return tensors._ta
@@ -381,6 +476,7 @@ class Context:
         self.lib = load_library()
         self.device = torch.device(device if device is not None else "cuda:0")
         idx = self.device.index if self.device.index is not None else 0
+        self._device = torch.device(self.device.type, idx)  # (as tensors name it)
         self.stream = torch.cuda.current_stream(self.device)
         h = C.c_void_p()
         rc = self.lib.inshr_create(C.byref(h), idx, C.c_void_p(self.stream.cuda_stream), scratch_bytes)
@@ -875,6 +971,167 @@ class Context:
         ca = _filled(CCodesOut, nT, packed=[x.data_ptr() for x in res], packed_words=words, bins=Kc)
         self._check(self.lib.inshr_reconstruct(self.h, pa, da, ca, nT))
         return res
+
+
+    # -- answers of a compressed checkpoint -------------------------------------------------
+    def _enter(self, *used):
+        """Where torch works on another stream than the context's: the context's waits for it and it for the context's
+        afterwards, the tensors (and layers) in use are kept from being reused too early, and what is allocated
+        meanwhile belongs to the context's stream."""
+        return _Turn(self.stream, used) if torch.cuda.current_stream(self.device) != self.stream else _NO_TURN
+
+    def _rows_of(self, t: torch.Tensor, cols: int, name: str):
+        if t.dim() != 2 or t.shape[1] != cols or t.dtype not in _TYPES or t.device != self._device:
+            raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor [rows, {cols}] on {self._device}")
+        return t.shape[0], _TYPES[t.dtype]
+
+    def linear(self, layer: QuantizedLayer, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None, want_pre: bool = False):
+        """act(x W^T + bias) + residual of x [rows, n_in] (float32, bfloat16 or float16; rows may lie apart), in x's
+        type; with want_pre also x W^T + bias, which linear_grad takes.  out may be the residual itself.  Returns
+        after enqueueing."""
+        rows, type_ = self._rows_of(x, layer.n_in, "x")
+        dev, dt, n_out = self._device, x.dtype, layer.n_out
+        cx = _matrix(x, rows, layer.n_in, dt, dev, "x")
+        cr = _matrix(residual, rows, n_out, dt, dev, "residual")
+        c = layer._c[type_]
+        need = layer._space.get((0, rows, type_))
+        if need is None:
+            b = C.c_uint64()
+            self._check(self.lib.inshr_linear_bound(C.byref(c), rows, C.byref(b)))
+            need = layer._space[0, rows, type_] = b.value
+        y = torch.empty((rows, n_out), dtype=dt, device=dev) if out is None else out
+        cy = _matrix(y, rows, n_out, dt, dev, "out")
+        pre = torch.empty((rows, n_out), dtype=dt, device=dev) if want_pre else None
+        cp = CMatrix(pre.data_ptr(), n_out) if want_pre else _NO_MATRIX
+        with self._enter(x, residual, y, pre, layer):
+            ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+            self._check(self.lib.inshr_linear(self.h, C.byref(c), cx, cr, cy, cp, rows,
+                                              ws.data_ptr() if need else None, need))
+        return (y, pre) if want_pre else y
+
+    def linear_grad(self, layer: QuantizedLayer, x: Optional[torch.Tensor], dy: torch.Tensor,
+                    pre: Optional[torch.Tensor] = None, want_dx: bool = True, want_dw: bool = True,
+                    want_dbias: bool = True):
+        """(dx, dw, dbias) of linear for dy [rows, n_out], the gradient of its result; dx in dy's type, dw float32 in
+        the layout of the weight (what quantize_sens takes), dbias float32 [n_out]; None for what is not wanted.  x is
+        needed for dw, pre for every activation but none.  Returns after enqueueing."""
+        rows, type_ = self._rows_of(dy, layer.n_out, "dy")
+        dev, dt, n_in, n_out = self._device, dy.dtype, layer.n_in, layer.n_out
+        if want_dw and x is None:
+            raise ValueError("dw needs x")
+        if pre is None and layer.activation != "none":
+            raise ValueError("the gradient of an activation needs pre")
+        cx = _matrix(x, rows, n_in, dt, dev, "x")
+        cd = _matrix(dy, rows, n_out, dt, dev, "dy")
+        cp = _matrix(pre, rows, n_out, dt, dev, "pre")
+        c = layer._c[type_]
+        key = (1, rows, type_, want_dx, want_dw)
+        need = layer._space.get(key)
+        if need is None:
+            b = C.c_uint64()
+            self._check(self.lib.inshr_linear_grad_bound(C.byref(c), rows, want_dx, want_dw, C.byref(b)))
+            need = layer._space[key] = b.value
+        dx = torch.empty((rows, n_in), dtype=dt, device=dev) if want_dx else None
+        dw = torch.empty((n_in, n_out) if layer.in_out else (n_out, n_in), dtype=torch.float32,
+                         device=dev) if want_dw else None
+        db = torch.empty(n_out, dtype=torch.float32, device=dev) if want_dbias else None
+        with self._enter(x, dy, pre, dx, dw, db, layer):
+            ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+            if rows or want_dw or want_dbias:
+                self._check(self.lib.inshr_linear_grad(
+                    self.h, C.byref(c), cx, cd, cp, _matrix(dx, rows, n_in, dt, dev, "dx"),
+                    dw.data_ptr() if want_dw else None, db.data_ptr() if want_dbias else None, rows,
+                    ws.data_ptr() if need else None, need))
+        return dx, dw, db
+
+    def top_logits(self, logits: torch.Tensor, k: int, temperature: float = 1.0, want_tail: bool = True) -> TopLogits:
+        """The k largest logits of every row [rows, n_vocab], largest first, equal ones by rising index, and the log of
+        the others' sum.  Returns after enqueueing."""
+        vocab = logits.shape[1] if logits.dim() == 2 else 0
+        rows, type_ = self._rows_of(logits, vocab, "logits")
+        dev = self._device
+        cl = _matrix(logits, rows, vocab, logits.dtype, dev, "logits")
+        if not 1 <= k <= vocab:
+            raise ValueError("k must lie in 1 .. n_vocab")
+        index = torch.empty((rows, k), dtype=torch.int32, device=dev)
+        value = torch.empty((rows, k), dtype=torch.float32, device=dev)
+        tail = torch.empty(rows, dtype=torch.float32, device=dev) if want_tail else None
+        with self._enter(logits, index, value, tail):
+            self._check(self.lib.inshr_top_logits(self.h, cl, type_, rows, vocab, k, temperature, index.data_ptr(),
+                                                  value.data_ptr(), tail.data_ptr() if want_tail else None))
+        return TopLogits(index, value, tail, temperature)
+
+    def _distill_in(self, logits, top):
+        vocab = logits.shape[1] if logits.dim() == 2 else 0
+        rows, type_ = self._rows_of(logits, vocab, "logits")
+        dev, k = self._device, top.index.shape[1] if top.index.dim() == 2 else 0
+        return rows, CDistillIn(_matrix(logits, rows, vocab, logits.dtype, dev, "logits"),
+                                _vector(top.index, (rows, k), torch.int32, dev, "index"),
+                                _vector(top.value, (rows, k), torch.float32, dev, "value"),
+                                _vector(top.tail, (rows,), torch.float32, dev, "tail"), rows, vocab, k, type_,
+                                top.temperature)
+
+    def distill(self, logits: torch.Tensor, top: TopLogits, want_saved: bool = True):
+        """(loss float32 [rows], saved): the divergence of the student's logits [rows, n_vocab] from what the teacher
+        says of them, and what distill_grad wants.  Returns after enqueueing."""
+        rows, c = self._distill_in(logits, top)
+        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        saved = torch.empty((rows, DISTILL_SAVED), dtype=torch.float64, device=logits.device) if want_saved else None
+        with self._enter(logits, top.index, top.value, top.tail, loss, saved):
+            self._check(self.lib.inshr_distill(self.h, C.byref(c), loss.data_ptr(),
+                                               saved.data_ptr() if want_saved else None))
+        return loss, saved
+
+    def distill_grad(self, logits: torch.Tensor, top: TopLogits, saved: torch.Tensor,
+                     grad_loss: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The gradient of the logits for grad_loss (float32 [rows], None: 1), in their type.  out may be the logits
+        themselves.  Returns after enqueueing."""
+        rows, c = self._distill_in(logits, top)
+        dev, vocab = logits.device, logits.shape[1]
+        cs = _vector(saved, (rows, DISTILL_SAVED), torch.float64, dev, "saved")
+        cg = _vector(grad_loss, (rows,), torch.float32, dev, "grad_loss")
+        grad = torch.empty((rows, vocab), dtype=logits.dtype, device=dev) if out is None else out
+        co = _matrix(grad, rows, vocab, logits.dtype, dev, "out")
+        with self._enter(logits, top.index, top.value, top.tail, saved, grad_loss, grad):
+            self._check(self.lib.inshr_distill_grad(self.h, C.byref(c), cs, cg, co))
+        return grad
+
+
+class _NoTurn:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *_):
+        pass
+
+
+_NO_TURN = _NoTurn()
+
+
+class _Turn:
+    """A call on the context's stream between what torch's current stream has done and will do."""
+
+    def __init__(self, stream, used):
+        self.stream, self.tensors = stream, []
+        for t in used:
+            if isinstance(t, QuantizedLayer):
+                self.tensors += [*t.q._bufs, t.bias]
+            else:
+                self.tensors.append(t)
+
+    def __enter__(self):
+        self.before = torch.cuda.current_stream(self.stream.device)
+        self.stream.wait_stream(self.before)
+        for t in self.tensors:
+            if t is not None:
+                t.record_stream(self.stream)
+        self.inner = torch.cuda.stream(self.stream)
+        self.inner.__enter__()
+
+    def __exit__(self, *e):
+        self.inner.__exit__(*e)
+        self.before.wait_stream(self.stream)
 
 
 # -- entropy stage of the delta: host memory, no device involved ------------------------------------

@@ -1,0 +1,119 @@
+// Descriptors of the operators that run layers from their compressed form and compare answers
+// (inshr_linear.hip, inshr_logits.hip), and what their kernels share.
+#pragma once
+#include "inshr_launch.h"
+
+namespace inshr {
+
+// element types of activations and logits; the numbers are those of the C ABI
+constexpr u32 TY_F32 = 0u, TY_BF16 = 1u, TY_F16 = 2u;
+// activations; the numbers are those of the C ABI
+constexpr u32 ACT_NONE = 0u, ACT_RELU = 1u, ACT_GELU = 2u, ACT_GELU_TANH = 3u, ACT_SILU = 4u;
+
+__host__ __device__ inline u64 elem_size(u32 type) { return type == TY_F32 ? 4u : 2u; }
+
+struct WDesc { // a weight as the quantizer left it, row-major [rows][cols]
+    const u32 *packed;      // the symbol stream as 32-bit words, n_words of them
+    const float *codebook;
+    const u32 *out_idx;
+    const void *out_val;    // fp32, or bfloat16 where val_bf16 is set
+    u64 n_words, n_outlier;
+    u32 rows, cols, w, K, val_bf16, pad;
+};
+
+struct Mat { // rows of a matrix in the caller's memory
+    void *p;
+    u64 stride; // elements between rows
+};
+
+struct LinearCall {
+    WDesc w;
+    const float *bias;
+    Mat x, residual, y, pre; // p == NULL: not given, not wanted
+    u64 rows;
+    u32 n_in, n_out, in_out, type, act;
+    char *ws;                // workspace, linear_space() bytes
+};
+struct LinearGradCall {
+    WDesc w;
+    Mat x, dy, pre, dx;
+    float *dw, *db;
+    u64 rows;
+    u32 n_in, n_out, in_out, type, act;
+    char *ws;                // workspace, linear_grad_space() bytes
+};
+u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type);
+u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw);
+hipError_t launch_linear(const LinearCall &c, hipStream_t s);
+hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s);
+
+constexpr u32 MAX_VOCAB = 1u << 18; // a bit per logit of a row fits into 32 KB of LDS
+constexpr u32 MAX_LISTED = 256u;
+struct LogitsCall {
+    Mat logits;
+    u64 rows;
+    u32 type, n_vocab, k;
+    float temperature;
+    const int *index;   // [rows][k]
+    const float *value; // [rows][k]
+    const float *tail;  // [rows] or NULL
+};
+hipError_t launch_top_logits(const LogitsCall &c, int *index, float *value, float *tail, hipStream_t s);
+hipError_t launch_distill(const LogitsCall &c, float *loss, double *saved, hipStream_t s);
+hipError_t launch_distill_grad(const LogitsCall &c, const double *saved, const float *g, const Mat &grad, hipStream_t s);
+
+// ------------------------------------------------------------------------------------------
+// elements
+// ------------------------------------------------------------------------------------------
+template <u32 TY> struct Elem;
+template <> struct Elem<TY_F32> {
+    typedef float type;
+    static __device__ __forceinline__ float get(float v) { return v; }
+    static __device__ __forceinline__ float put(float v) { return v; }
+};
+template <> struct Elem<TY_BF16> {
+    typedef u16 type;
+    static __device__ __forceinline__ float get(u16 v) { return __uint_as_float((u32)v << 16); }
+    static __device__ __forceinline__ u16 put(float v) // to nearest even, NaN stays NaN
+    {
+        const u32 b = __float_as_uint(v);
+        if ((b & 0x7fffffffu) > 0x7f800000u) return (u16)(b >> 16 | 0x40u);
+        return (u16)((b + 0x7fffu + (b >> 16 & 1u)) >> 16);
+    }
+};
+template <> struct Elem<TY_F16> {
+    typedef _Float16 type;
+    static __device__ __forceinline__ float get(_Float16 v) { return (float)v; }
+    static __device__ __forceinline__ _Float16 put(float v) { return (_Float16)v; }
+};
+
+typedef u32 u4_16 __attribute__((ext_vector_type(4)));
+
+// Eight consecutive elements, of which `left` exist (the others read as 0).  wide: the address is 16-byte aligned.
+template <u32 TY>
+__device__ __forceinline__ void load8(const GLOBAL_AS typename Elem<TY>::type *p, bool wide, u32 left, float (&v)[8])
+{
+    typedef typename Elem<TY>::type T;
+    if (wide && left >= 8u) {
+        union {
+            u4_16 q[sizeof(T) / 2];
+            T e[8];
+        } x;
+#pragma unroll
+        for (u32 i = 0; i < sizeof(T) / 2; i++) x.q[i] = ((const GLOBAL_AS u4_16 *)p)[i];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = Elem<TY>::get(x.e[i]);
+    } else {
+#pragma unroll
+        for (u32 i = 0; i < 8u; i++) v[i] = i < left ? Elem<TY>::get(p[i]) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
+} // namespace inshr

@@ -2,6 +2,7 @@
 // kernel sequencing.  No arithmetic of the method runs here.
 #include "../../include/inshr.h"
 #include "inshr_launch.h"
+#include "inshr_answer.h"
 #include "inshr_sketch.h"
 
 #include <algorithm>
@@ -2374,6 +2375,249 @@ int inshr_reconstruct(inshr_ctx *c, const inshr_codes *prev, const inshr_delta_o
     }
     if (f & RF_GROUPS) return INSHR_E_SHAPE;
     if (f & RF_DELTA) return INSHR_E_ARG;
+    return INSHR_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// answers of a compressed checkpoint
+// ------------------------------------------------------------------------------------------
+namespace {
+
+constexpr uint64_t MAX_ROWS = 1ull << 22, MAX_DIM = 1ull << 30;
+
+struct OnDevice { // the context's device for the length of a call
+    int before = -1;
+    hipError_t err;
+    explicit OnDevice(int device)
+    {
+        err = hipGetDevice(&before);
+        if (err == hipSuccess && before != device) err = hipSetDevice(device);
+        if (before == device) before = -1;
+    }
+    ~OnDevice()
+    {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+bool aligned(const void *p, uint64_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+// A matrix that is wanted or may be missing; rows that are written must not overlap.
+bool matrix_ok(const inshr_matrix &m, uint32_t type, uint64_t cols, bool needed, bool written)
+{
+    if (!m.data) return !needed;
+    if (!aligned(m.data, elem_size(type))) return false;
+    return written ? m.stride >= cols && m.stride < (1ull << 40) : m.stride < (1ull << 40);
+}
+Mat mat(const inshr_matrix &m) { return {m.data, m.stride}; }
+
+int layer_of(const inshr_layer *layer, uint64_t rows, WDesc &w)
+{
+    if (!layer) return INSHR_E_ARG;
+    const inshr_dequant_in &q = layer->weight;
+    inshr_codes as_codes;
+    as_codes.bits = q.bits;
+    as_codes.bins = q.bins;
+    uint32_t K = 0;
+    if (codes_bins(as_codes, K)) return INSHR_E_CONFIG;
+    if (layer->type > INSHR_F16 || layer->activation > INSHR_ACT_SILU || layer->reserved || rows > MAX_ROWS) return INSHR_E_ARG;
+    if (layer->n_out == 0 || layer->n_in == 0 || layer->n_out > MAX_DIM || layer->n_in > MAX_DIM) return INSHR_E_ARG;
+    if (q.n != (uint64_t)layer->n_out * layer->n_in || q.n >= (1ull << 32)) return INSHR_E_ARG;
+    if (!q.packed || !q.codebook || !aligned(q.packed, 8) || !aligned(q.codebook, 4) || !aligned(layer->bias, 4)) return INSHR_E_ARG;
+    if (q.n_outlier && (!q.outlier_idx || !q.outlier_val)) return INSHR_E_ARG;
+    if (!aligned(q.outlier_idx, 4) || !aligned(q.outlier_val, q.protected_bf16 ? 2 : 4)) return INSHR_E_ARG;
+    if (q.n_outlier > q.n) return INSHR_E_SHAPE;
+    memset(&w, 0, sizeof(w));
+    w.packed = (const u32 *)q.packed;
+    w.codebook = q.codebook;
+    w.out_idx = q.outlier_idx;
+    w.out_val = q.outlier_val;
+    w.n_outlier = q.n_outlier;
+    w.rows = layer->in_out ? layer->n_in : layer->n_out;
+    w.cols = layer->in_out ? layer->n_out : layer->n_in;
+    w.K = K;
+    w.w = symbol_bits(K);
+    w.n_words = (q.n * w.w + 63) / 64 * 2;
+    w.val_bf16 = q.protected_bf16 ? 1u : 0u;
+    return INSHR_OK;
+}
+
+int workspace_ok(inshr_ctx *c, const char *call, const void *ws, uint64_t have, uint64_t need)
+{
+    if (need && (!ws || !aligned(ws, 256))) return INSHR_E_ARG;
+    if (have < need) {
+        c->last_err = std::string(call) + ": the workspace has " + std::to_string(have) + " bytes, the call needs " + std::to_string(need);
+        return INSHR_E_CAPACITY;
+    }
+    return INSHR_OK;
+}
+
+int logits_of(const inshr_matrix &m, uint32_t type, uint64_t rows, uint32_t n_vocab, uint32_t k, float temperature, LogitsCall &l)
+{
+    if (type > INSHR_F16 || rows > MAX_ROWS || n_vocab == 0 || n_vocab > INSHR_MAX_VOCAB) return INSHR_E_ARG;
+    if (k == 0 || k > INSHR_MAX_LISTED || k > n_vocab) return INSHR_E_ARG;
+    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return INSHR_E_ARG;
+    if (rows && !matrix_ok(m, type, n_vocab, true, false)) return INSHR_E_ARG;
+    memset(&l, 0, sizeof(l));
+    l.logits = mat(m);
+    l.rows = rows;
+    l.type = type;
+    l.n_vocab = n_vocab;
+    l.k = k;
+    l.temperature = temperature;
+    return INSHR_OK;
+}
+int distill_of(const inshr_distill_in *in, LogitsCall &l)
+{
+    if (!in) return INSHR_E_ARG;
+    const int rc = logits_of(in->logits, in->type, in->rows, in->n_vocab, in->k, in->temperature, l);
+    if (rc) return rc;
+    if (in->rows && (!in->index || !in->value)) return INSHR_E_ARG;
+    if (!aligned(in->index, 4) || !aligned(in->value, 4) || !aligned(in->tail, 4)) return INSHR_E_ARG;
+    l.index = in->index;
+    l.value = in->value;
+    l.tail = in->tail;
+    return INSHR_OK;
+}
+
+} // namespace
+
+int inshr_linear_bound(const inshr_layer *layer, uint64_t rows, uint64_t *workspace_bytes)
+{
+    if (!workspace_bytes) return INSHR_E_ARG;
+    WDesc w;
+    const int rc = layer_of(layer, rows, w);
+    if (rc) return rc;
+    *workspace_bytes = linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type);
+    return INSHR_OK;
+}
+
+int inshr_linear(inshr_ctx *c, const inshr_layer *layer, inshr_matrix x, inshr_matrix residual, inshr_matrix y,
+                 inshr_matrix pre, uint64_t rows, void *workspace, uint64_t workspace_bytes)
+{
+    if (!c) return INSHR_E_ARG;
+    LinearCall call;
+    memset(&call, 0, sizeof(call));
+    int rc = layer_of(layer, rows, call.w);
+    if (rc) return rc;
+    if (rows == 0) return INSHR_OK;
+    if (!matrix_ok(x, layer->type, layer->n_in, true, false) || !matrix_ok(residual, layer->type, layer->n_out, false, false) ||
+        !matrix_ok(y, layer->type, layer->n_out, true, true) || !matrix_ok(pre, layer->type, layer->n_out, false, true))
+        return INSHR_E_ARG;
+    if (residual.data == y.data && residual.stride != y.stride) return INSHR_E_ARG;
+    rc = workspace_ok(c, "inshr_linear", workspace, workspace_bytes,
+                      linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type));
+    if (rc) return rc;
+    call.bias = layer->bias;
+    call.x = mat(x);
+    call.residual = mat(residual);
+    call.y = mat(y);
+    call.pre = mat(pre);
+    call.rows = rows;
+    call.n_in = layer->n_in;
+    call.n_out = layer->n_out;
+    call.in_out = layer->in_out ? 1u : 0u;
+    call.type = layer->type;
+    call.act = layer->activation;
+    call.ws = (char *)workspace;
+    OnDevice dev(c->device);
+    HIPCHK(c, dev.err);
+    HIPCHK(c, launch_linear(call, c->stream));
+    return INSHR_OK;
+}
+
+int inshr_linear_grad_bound(const inshr_layer *layer, uint64_t rows, uint32_t want_dx,
+                            uint32_t want_dw, uint64_t *workspace_bytes)
+{
+    if (!workspace_bytes) return INSHR_E_ARG;
+    WDesc w;
+    const int rc = layer_of(layer, rows, w);
+    if (rc) return rc;
+    *workspace_bytes = linear_grad_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->activation,
+                                         want_dx != 0, want_dw != 0);
+    return INSHR_OK;
+}
+
+int inshr_linear_grad(inshr_ctx *c, const inshr_layer *layer, inshr_matrix x, inshr_matrix dy, inshr_matrix pre,
+                      inshr_matrix dx, float *dw, float *dbias, uint64_t rows, void *workspace,
+                      uint64_t workspace_bytes)
+{
+    if (!c || (!dx.data && !dw && !dbias)) return INSHR_E_ARG;
+    LinearGradCall call;
+    memset(&call, 0, sizeof(call));
+    int rc = layer_of(layer, rows, call.w);
+    if (rc) return rc;
+    const bool bent = layer->activation != INSHR_ACT_NONE;
+    if (rows && (!matrix_ok(x, layer->type, layer->n_in, dw != nullptr, false) || !matrix_ok(dy, layer->type, layer->n_out, true, false) ||
+                 !matrix_ok(pre, layer->type, layer->n_out, bent, false) || !matrix_ok(dx, layer->type, layer->n_in, false, true)))
+        return INSHR_E_ARG;
+    if (!aligned(dw, 4) || !aligned(dbias, 4)) return INSHR_E_ARG;
+    rc = workspace_ok(c, "inshr_linear_grad", workspace, workspace_bytes,
+                      linear_grad_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->activation,
+                                        dx.data != nullptr, dw != nullptr));
+    if (rc) return rc;
+    call.x = mat(x);
+    call.dy = mat(dy);
+    call.pre = mat(pre);
+    call.dx = mat(dx);
+    call.dw = dw;
+    call.db = dbias;
+    call.rows = rows;
+    call.n_in = layer->n_in;
+    call.n_out = layer->n_out;
+    call.in_out = layer->in_out ? 1u : 0u;
+    call.type = layer->type;
+    call.act = layer->activation;
+    call.ws = (char *)workspace;
+    OnDevice dev(c->device);
+    HIPCHK(c, dev.err);
+    HIPCHK(c, launch_linear_grad(call, c->stream));
+    return INSHR_OK;
+}
+
+int inshr_top_logits(inshr_ctx *c, inshr_matrix logits, uint32_t type, uint64_t rows, uint32_t n_vocab, uint32_t k,
+                     float temperature, int32_t *index, float *value, float *tail)
+{
+    if (!c) return INSHR_E_ARG;
+    LogitsCall call;
+    const int rc = logits_of(logits, type, rows, n_vocab, k, temperature, call);
+    if (rc) return rc;
+    if (rows == 0) return INSHR_OK;
+    if (!index || !value || !aligned(index, 4) || !aligned(value, 4) || !aligned(tail, 4)) return INSHR_E_ARG;
+    OnDevice dev(c->device);
+    HIPCHK(c, dev.err);
+    HIPCHK(c, launch_top_logits(call, index, value, tail, c->stream));
+    return INSHR_OK;
+}
+
+int inshr_distill(inshr_ctx *c, const inshr_distill_in *in, float *loss, double *saved)
+{
+    if (!c) return INSHR_E_ARG;
+    LogitsCall call;
+    const int rc = distill_of(in, call);
+    if (rc) return rc;
+    if (in->rows == 0) return INSHR_OK;
+    if (!loss || !aligned(loss, 4) || !aligned(saved, 8)) return INSHR_E_ARG;
+    OnDevice dev(c->device);
+    HIPCHK(c, dev.err);
+    HIPCHK(c, launch_distill(call, loss, saved, c->stream));
+    return INSHR_OK;
+}
+
+int inshr_distill_grad(inshr_ctx *c, const inshr_distill_in *in, const double *saved, const float *grad_loss,
+                       inshr_matrix grad)
+{
+    if (!c) return INSHR_E_ARG;
+    LogitsCall call;
+    const int rc = distill_of(in, call);
+    if (rc) return rc;
+    if (in->rows == 0) return INSHR_OK;
+    if (!saved || !aligned(saved, 8) || !aligned(grad_loss, 4)) return INSHR_E_ARG;
+    if (!matrix_ok(grad, in->type, in->n_vocab, true, true)) return INSHR_E_ARG;
+    if (grad.data == in->logits.data && grad.stride != in->logits.stride) return INSHR_E_ARG;
+    OnDevice dev(c->device);
+    HIPCHK(c, dev.err);
+    HIPCHK(c, launch_distill_grad(call, saved, grad_loss, mat(grad), c->stream));
     return INSHR_OK;
 }
 
