@@ -45,6 +45,9 @@ struct LinearGradCall {
 u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type);
 u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw);
 hipError_t launch_linear(const LinearCall &c, hipStream_t s);
+hipError_t launch_few(const LinearCall &c, hipStream_t s); // few rows: no workspace
+// FEWRULE
+inline bool is_few(u64 rows) { return rows <= 64; }
 hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s);
 
 constexpr u32 MAX_VOCAB = 1u << 18; // a bit per logit of a row fits into 32 KB of LDS

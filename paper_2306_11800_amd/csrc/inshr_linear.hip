@@ -9,77 +9,9 @@
 //   2 passes h h + h l          for fp16 results: fp16 activations are exact in h, the weight keeps 22 bits
 //   3 passes h h + h l + l h    for fp32 results: what is left out, l l, is 2^-22 of the product
 // (three planes of bfloat16 would need six passes for fp32, and two for bfloat16 results).
-#include "inshr_answer.h"
+#include "inshr_product.h"
 
 namespace inshr {
-
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-typedef float f4 __attribute__((ext_vector_type(4)));
-
-// ------------------------------------------------------------------------------------------
-// scales
-// ------------------------------------------------------------------------------------------
-// The power of two that brings a largest magnitude (bits of |x|) into [2^14, 2^15), and its inverse; both normal.  An
-// infinity counts as the largest finite exponent: it stays infinite under any scale.
-__device__ __forceinline__ void scale_of(u32 mag, float &s, float &inv)
-{
-    u32 e = mag >> 23;
-    e = e > 254u ? 254u : e;
-    const u32 sb = e < 15u ? 253u : 268u - e;
-    s = __uint_as_float(sb << 23);
-    inv = __uint_as_float((254u - sb) << 23);
-}
-__device__ __forceinline__ u32 mag_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-__device__ __forceinline__ u32 wave_max_u(u32 v)
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        const u32 o = __shfl_xor(v, d);
-        v = v > o ? v : o;
-    }
-    return v;
-}
-// (magnitudes of infinities and NaN say nothing of the finite values' scale)
-__device__ __forceinline__ u32 finite_mag(float x)
-{
-    const u32 m = mag_bits(x);
-    return m < 0x7f800000u ? m : 0u;
-}
-
-// ------------------------------------------------------------------------------------------
-// activations
-// ------------------------------------------------------------------------------------------
-__device__ __forceinline__ float act_of(float a, u32 act)
-{
-    switch (act) {
-    case ACT_RELU: return a > 0.0f ? a : a != a ? a : 0.0f;
-    case ACT_GELU: return 0.5f * a * (1.0f + erff(a * 0.70710678118654752f));
-    case ACT_GELU_TANH: { // 0.5 a (1 + tanh u) = a / (1 + e^(-2u))
-        const float u = 0.79788456080286536f * (a + 0.044715f * a * a * a);
-        return a / (1.0f + expf(-2.0f * u));
-    }
-    case ACT_SILU: return a / (1.0f + expf(-a));
-    default: return a;
-    }
-}
-__device__ __forceinline__ float act_grad(float a, u32 act)
-{
-    switch (act) {
-    case ACT_RELU: return a > 0.0f ? 1.0f : a != a ? a : 0.0f;
-    case ACT_GELU: return 0.5f * (1.0f + erff(a * 0.70710678118654752f)) + a * 0.39894228040143268f * expf(-0.5f * a * a);
-    case ACT_GELU_TANH: {
-        const float u = 0.79788456080286536f * (a + 0.044715f * a * a * a);
-        const float t = tanhf(u);
-        return 0.5f * (1.0f + t) + 0.5f * a * (1.0f - t * t) * 0.79788456080286536f * (1.0f + 0.134145f * a * a);
-    }
-    case ACT_SILU: {
-        const float g = 1.0f / (1.0f + expf(-a));
-        return g * (1.0f + a * (1.0f - g));
-    }
-    default: return 1.0f;
-    }
-}
 
 // ------------------------------------------------------------------------------------------
 // planes of an operand whose reduction runs along its rows
@@ -210,11 +142,6 @@ __global__ __launch_bounds__(256) void k_col_planes(PlaneSrc src, const float *_
 // ------------------------------------------------------------------------------------------
 constexpr u32 WMAX_PARTS = 64;
 
-__device__ __forceinline__ float protected_value(const WDesc &w, u64 j)
-{
-    return w.val_bf16 ? __uint_as_float((u32)((const GLOBAL_AS u16 *)w.out_val)[j] << 16) : ((const GLOBAL_AS float *)w.out_val)[j];
-}
-
 // largest magnitudes of the centres and of parts of the protected list
 __global__ __launch_bounds__(256) void k_weight_max(WDesc w, u32 *__restrict__ part)
 {
@@ -245,13 +172,6 @@ __device__ __forceinline__ u32 symbol_at(const WDesc &w, u64 i)
     const u64 bit = i * w.w, at = bit >> 5;
     const u32 lo = gptr(w.packed)[at], hi = at + 1 < w.n_words ? gptr(w.packed)[at + 1] : 0u;
     return __builtin_amdgcn_alignbit(hi, lo, (u32)bit & 31u) & ((1u << w.w) - 1u);
-}
-
-// Values of the symbols: 0 for pruned, 0 for protected (their values follow from the list), the centres, and NaN for
-// what is no symbol of the codebook.
-__device__ __forceinline__ float symbol_value(const WDesc &w, u32 s)
-{
-    return s < 2u ? 0.0f : s < w.K + 2u ? gptr(w.codebook)[s - 2u] : __uint_as_float(0x7fc00000u);
 }
 
 // Planes [rows][Cp] (T == false) or, transposed, [cols][Rp]; padding of the reduction is zero.
@@ -322,26 +242,9 @@ struct Gemm {
     u32 pa, pb;              // plane of pass i: bit i
     const float *inv_a, *inv_b; // per row; inv_b NULL: the weight's
     const u32 *wpart;
-    const float *bias;
-    Mat residual, out, pre;
-    u32 type, act;           // of out
+    Finish end;
+    u32 type;                // of the results
 };
-
-template <u32 TY>
-__device__ __forceinline__ void epilogue4(const Gemm &g, u32 m, u32 n, const f4 &v)
-{
-    typedef typename Elem<TY>::type T;
-#pragma unroll
-    for (u32 i = 0; i < 4u; i++) {
-        if (n + i >= g.N) break;
-        float a = v[i];
-        if (g.bias) a += gptr(g.bias)[n + i];
-        if (g.pre.p) ((GLOBAL_AS T *)g.pre.p)[(u64)m * g.pre.stride + n + i] = Elem<TY>::put(a);
-        float y = act_of(a, g.act);
-        if (g.residual.p) y += Elem<TY>::get(((const GLOBAL_AS T *)g.residual.p)[(u64)m * g.residual.stride + n + i]);
-        ((GLOBAL_AS T *)g.out.p)[(u64)m * g.out.stride + n + i] = Elem<TY>::put(y);
-    }
-}
 
 template <u32 TY>
 __global__ __launch_bounds__(256) void k_product(Gemm g)
@@ -400,7 +303,7 @@ __global__ __launch_bounds__(256) void k_product(Gemm g)
             f4 v = acc[i][j];
 #pragma unroll
             for (u32 t = 0; t < 4u; t++) v[t] = v[t] * inv_a * (g.inv_b ? (n + t < g.N ? gptr(g.inv_b)[n + t] : 0.0f) : inv_w);
-            epilogue4<TY>(g, m, n, v);
+            epilogue4<TY>(g.end, m, n, v);
         }
     }
 }
@@ -569,7 +472,7 @@ struct GradRoom {
 
 u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type)
 {
-    return rows ? LinearRoom(rows, n_in, n_out, type).bytes : 0;
+    return is_few(rows) ? 0 : LinearRoom(rows, n_in, n_out, type).bytes;
 }
 u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw)
 {
@@ -578,6 +481,7 @@ u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 a
 
 hipError_t launch_linear(const LinearCall &c, hipStream_t s)
 {
+    if (is_few(c.rows)) return launch_few(c, s);
     const LinearRoom r(c.rows, c.n_in, c.n_out, c.type);
     const PlaneSrc x = {c.x.p, nullptr, c.x.stride, 0, (u32)c.rows, c.n_in, ACT_NONE};
     row_planes(x, c.type, r.x, c.ws, s);
@@ -587,12 +491,8 @@ hipError_t launch_linear(const LinearCall &c, hipStream_t s)
     g.N = c.n_out;
     g.inv_a = (const float *)(c.ws + r.x.inv);
     g.wpart = (const u32 *)(c.ws + r.part);
-    g.bias = c.bias;
-    g.residual = c.residual;
-    g.out = c.y;
-    g.pre = c.pre;
+    g.end = {c.bias, c.residual, c.y, c.pre, c.n_out, c.act};
     g.type = c.type;
-    g.act = c.act;
     product(g, r.x, r.w, c.ws, s);
     return hipGetLastError();
 }
@@ -626,7 +526,7 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
         g.N = c.n_in;
         g.inv_a = (const float *)(c.ws + r.dr.inv);
         g.wpart = (const u32 *)(c.ws + r.part);
-        g.out = c.dx;
+        g.end = {nullptr, {}, c.dx, {}, c.n_in, ACT_NONE};
         g.type = c.type;
         product(g, r.dr, r.w, c.ws, s);
     }
@@ -641,7 +541,7 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
         g.N = c.in_out ? c.n_out : c.n_in;
         g.inv_a = (const float *)(c.ws + a.inv);
         g.inv_b = (const float *)(c.ws + b.inv);
-        g.out = {c.dw, g.N};
+        g.end = {nullptr, {}, {c.dw, g.N}, {}, g.N, ACT_NONE};
         g.type = TY_F32;
         product(g, a, b, c.ws, s);
     }

@@ -1,0 +1,116 @@
+// What the kernels of the products share: vector types, scales, activations, what follows a sum.
+#pragma once
+#include "inshr_answer.h"
+
+namespace inshr {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------------------------------------
+// scales
+// ------------------------------------------------------------------------------------------
+// The power of two that brings a largest magnitude (bits of |x|) into [2^14, 2^15), and its inverse; both normal.  An
+// infinity counts as the largest finite exponent: it stays infinite under any scale.
+__device__ __forceinline__ void scale_of(u32 mag, float &s, float &inv)
+{
+    u32 e = mag >> 23;
+    e = e > 254u ? 254u : e;
+    const u32 sb = e < 15u ? 253u : 268u - e;
+    s = __uint_as_float(sb << 23);
+    inv = __uint_as_float((254u - sb) << 23);
+}
+__device__ __forceinline__ u32 mag_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ u32 wave_max_u(u32 v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const u32 o = __shfl_xor(v, d);
+        v = v > o ? v : o;
+    }
+    return v;
+}
+// (magnitudes of infinities and NaN say nothing of the finite values' scale)
+__device__ __forceinline__ u32 finite_mag(float x)
+{
+    const u32 m = mag_bits(x);
+    return m < 0x7f800000u ? m : 0u;
+}
+
+// ------------------------------------------------------------------------------------------
+// activations
+// ------------------------------------------------------------------------------------------
+__device__ __forceinline__ float act_of(float a, u32 act)
+{
+    switch (act) {
+    case ACT_RELU: return a > 0.0f ? a : a != a ? a : 0.0f;
+    case ACT_GELU: return 0.5f * a * (1.0f + erff(a * 0.70710678118654752f));
+    case ACT_GELU_TANH: { // 0.5 a (1 + tanh u) = a / (1 + e^(-2u))
+        const float u = 0.79788456080286536f * (a + 0.044715f * a * a * a);
+        return a / (1.0f + expf(-2.0f * u));
+    }
+    case ACT_SILU: return a / (1.0f + expf(-a));
+    default: return a;
+    }
+}
+__device__ __forceinline__ float act_grad(float a, u32 act)
+{
+    switch (act) {
+    case ACT_RELU: return a > 0.0f ? 1.0f : a != a ? a : 0.0f;
+    case ACT_GELU: return 0.5f * (1.0f + erff(a * 0.70710678118654752f)) + a * 0.39894228040143268f * expf(-0.5f * a * a);
+    case ACT_GELU_TANH: {
+        const float u = 0.79788456080286536f * (a + 0.044715f * a * a * a);
+        const float t = tanhf(u);
+        return 0.5f * (1.0f + t) + 0.5f * a * (1.0f - t * t) * 0.79788456080286536f * (1.0f + 0.134145f * a * a);
+    }
+    case ACT_SILU: {
+        const float g = 1.0f / (1.0f + expf(-a));
+        return g * (1.0f + a * (1.0f - g));
+    }
+    default: return 1.0f;
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// a weight's values
+// ------------------------------------------------------------------------------------------
+__device__ __forceinline__ float protected_value(const WDesc &w, u64 j)
+{
+    return w.val_bf16 ? __uint_as_float((u32)((const GLOBAL_AS u16 *)w.out_val)[j] << 16) : ((const GLOBAL_AS float *)w.out_val)[j];
+}
+
+// Values of the symbols: 0 for pruned, 0 for protected (their values follow from the list), the centres, and NaN for
+// what is no symbol of the codebook.
+__device__ __forceinline__ float symbol_value(const WDesc &w, u32 s)
+{
+    return s < 2u ? 0.0f : s < w.K + 2u ? gptr(w.codebook)[s - 2u] : __uint_as_float(0x7fc00000u);
+}
+
+// ------------------------------------------------------------------------------------------
+// what follows a sum
+// ------------------------------------------------------------------------------------------
+struct Finish {
+    const float *bias;
+    Mat residual, out, pre;
+    u32 N, act;
+};
+
+// Results (m, n) .. (m, n + 3), the columns past N left out.
+template <u32 TY>
+__device__ __forceinline__ void epilogue4(const Finish &g, u32 m, u32 n, const f4 &v)
+{
+    typedef typename Elem<TY>::type T;
+#pragma unroll
+    for (u32 i = 0; i < 4u; i++) {
+        if (n + i >= g.N) break;
+        float a = v[i];
+        if (g.bias) a += gptr(g.bias)[n + i];
+        if (g.pre.p) ((GLOBAL_AS T *)g.pre.p)[(u64)m * g.pre.stride + n + i] = Elem<TY>::put(a);
+        float y = act_of(a, g.act);
+        if (g.residual.p) y += Elem<TY>::get(((const GLOBAL_AS T *)g.residual.p)[(u64)m * g.residual.stride + n + i]);
+        ((GLOBAL_AS T *)g.out.p)[(u64)m * g.out.stride + n + i] = Elem<TY>::put(y);
+    }
+}
+
+} // namespace inshr
