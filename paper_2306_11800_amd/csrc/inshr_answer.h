@@ -91,32 +91,58 @@ template <> struct Elem<TY_F16> {
 };
 
 typedef u32 u4_16 __attribute__((ext_vector_type(4)));
+// 16 bytes at an address aligned to an element of E bytes: one instruction all the same
+template <u32 E> struct Any16;
+template <> struct Any16<2> { typedef u32 type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct Any16<4> { typedef u32 type __attribute__((ext_vector_type(4), aligned(4))); };
 
-// Eight consecutive elements, of which `left` exist (the others read as 0).  wide: the address is 16-byte aligned.
+// Eight consecutive elements as they lie in memory.
+template <u32 TY> union Raw8 {
+    typedef typename Elem<TY>::type T;
+    u4_16 q[sizeof(T) / 2];
+    T e[8];
+    __device__ __forceinline__ Raw8() {}
+    __device__ __forceinline__ float operator[](int i) const { return Elem<TY>::get(e[i]); }
+};
+// `left` of them exist, the others read as 0.
 template <u32 TY>
-__device__ __forceinline__ void load8(const GLOBAL_AS typename Elem<TY>::type *p, bool wide, u32 left, float (&v)[8])
+__device__ __forceinline__ Raw8<TY> load_raw8(const GLOBAL_AS typename Elem<TY>::type *p, u32 left)
 {
     typedef typename Elem<TY>::type T;
-    if (wide && left >= 8u) {
-        union {
-            u4_16 q[sizeof(T) / 2];
-            T e[8];
-        } x;
+    typedef typename Any16<sizeof(T)>::type V;
+    Raw8<TY> x;
+    if (left >= 8u) {
 #pragma unroll
-        for (u32 i = 0; i < sizeof(T) / 2; i++) x.q[i] = ((const GLOBAL_AS u4_16 *)p)[i];
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = Elem<TY>::get(x.e[i]);
+        for (u32 i = 0; i < sizeof(T) / 2; i++) x.q[i] = ((const GLOBAL_AS V *)p)[i];
     } else {
 #pragma unroll
-        for (u32 i = 0; i < 8u; i++) v[i] = i < left ? Elem<TY>::get(p[i]) : 0.0f;
+        for (u32 i = 0; i < 8u; i++) x.e[i] = i < left ? p[i] : (T)0;
     }
+    return x;
 }
-
-__device__ __forceinline__ float wave_max(float v)
+template <u32 TY>
+__device__ __forceinline__ void load8(const GLOBAL_AS typename Elem<TY>::type *p, u32 left, float (&v)[8])
 {
+    const Raw8<TY> x = load_raw8<TY>(p, left);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    for (int i = 0; i < 8; i++) v[i] = x[i];
+}
+template <u32 TY>
+__device__ __forceinline__ void store8(GLOBAL_AS typename Elem<TY>::type *p, u32 left, const float (&v)[8])
+{
+    typedef typename Elem<TY>::type T;
+    typedef typename Any16<sizeof(T)>::type V;
+    Raw8<TY> x;
+#pragma unroll
+    for (int i = 0; i < 8; i++) x.e[i] = Elem<TY>::put(v[i]);
+    if (left >= 8u) {
+#pragma unroll
+        for (u32 i = 0; i < sizeof(T) / 2; i++) ((GLOBAL_AS V *)p)[i] = x.q[i];
+    } else {
+#pragma unroll
+        for (u32 i = 0; i < 8u; i++)
+            if (i < left) p[i] = x.e[i];
+    }
 }
 
 } // namespace inshr

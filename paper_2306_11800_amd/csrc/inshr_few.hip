@@ -132,11 +132,11 @@ template <u32 TY> struct Xs {
     Frag p[N];
 };
 template <u32 TY>
-__device__ __forceinline__ void load_xs(const GLOBAL_AS typename Elem<TY>::type *p, bool wide, u32 left, Xs<TY> &x)
+__device__ __forceinline__ void load_xs(const GLOBAL_AS typename Elem<TY>::type *p, u32 left, Xs<TY> &x)
 {
     if constexpr (TY == TY_F32) {
         float v[8];
-        load8<TY>(p, wide, left, v);
+        load8<TY>(p, left, v);
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             u32 h[2], m[2], l[2];
@@ -153,17 +153,7 @@ __device__ __forceinline__ void load_xs(const GLOBAL_AS typename Elem<TY>::type 
             x.p[2].u[i] = high_halves(l[0], l[1]);
         }
     } else {
-        if (wide && left >= 8u) {
-            x.p[0].q = *(const GLOBAL_AS u4_16 *)p;
-        } else {
-            union {
-                typename Elem<TY>::type e[8];
-                Frag f;
-            } y;
-#pragma unroll
-            for (u32 i = 0; i < 8u; i++) y.e[i] = i < left ? p[i] : (typename Elem<TY>::type)0;
-            x.p[0] = y.f;
-        }
+        x.p[0].q = load_raw8<TY>(p, left).q[0];
     }
 }
 template <u32 TY>
@@ -329,11 +319,9 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
         const u64 row_bit = (u64)min(n0 + i, f.n_out - 1u) * K * W;
         const u32 mine = lane_copy<TY, W>();
         const GLOBAL_AS T *x[MT];
-        bool wide = true;
 #pragma unroll
         for (int t = 0; t < MT; t++) {
             x[t] = (const GLOBAL_AS T *)f.x.p + (u64)min(m0 + 16u * t + i, f.rows - 1u) * f.x.stride;
-            wide = wide && ((u64)x[t] & 15u) == 0u;
         }
         for (u32 k0 = wave * 128u; k0 < K; k0 += waves * 128u) {
             const u32 k = k0 + 32u * g, left = k < K ? K - k : 0u;
@@ -362,7 +350,7 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
                     Xs<TY> v;
-                    load_xs<TY>(x[t] + k + 8 * s, wide, left > 8u * s ? left - 8u * s : 0u, v);
+                    load_xs<TY>(x[t] + k + 8 * s, left > 8u * s ? left - 8u * s : 0u, v);
                     acc[t] = multiply<TY>(w, v, acc[t]);
                 }
             }
@@ -401,11 +389,9 @@ __global__ __launch_bounds__(1024) void k_few_cols(Few f)
     const u32 i = lane & 15u, g = lane >> 4, K = f.n_in;
     const u32 mine = lane_copy<TY, W>();
     const GLOBAL_AS T *x[MT];
-    bool wide = true;
 #pragma unroll
     for (int t = 0; t < MT; t++) {
         x[t] = (const GLOBAL_AS T *)f.x.p + (u64)min(m0 + 16u * t + i, f.rows - 1u) * f.x.stride;
-        wide = wide && ((u64)x[t] & 15u) == 0u;
     }
     f4 acc[MT][R] = {};
     const u64 row_bits = (u64)f.n_out * W, run_bit = (u64)(n0 + i * R) * W;
@@ -425,7 +411,7 @@ __global__ __launch_bounds__(1024) void k_few_cols(Few f)
         }
         Xs<TY> v[MT];
 #pragma unroll
-        for (int t = 0; t < MT; t++) load_xs<TY>(x[t] + k, wide, left, v[t]);
+        for (int t = 0; t < MT; t++) load_xs<TY>(x[t] + k, left, v[t]);
 #pragma unroll
         for (int q = 0; q < R; q++) {
             Parts<TY> w;

@@ -33,12 +33,11 @@ __global__ __launch_bounds__(256) void k_row_planes(PlaneSrc src, _Float16 *__re
     typedef typename Elem<TY>::type T;
     const u64 r = blockIdx.x;
     const GLOBAL_AS T *p = (const GLOBAL_AS T *)src.p + r * src.stride;
-    const bool wide = ((u64)p & 15u) == 0u;
     __shared__ u32 red[4];
     u32 m = 0u;
     for (u32 c = threadIdx.x * 8u; c < src.cols; c += 2048u) {
         float v[8];
-        load8<TY>(p + c, wide, src.cols - c, v);
+        load8<TY>(p + c, src.cols - c, v);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const u32 f = finite_mag(v[i]);
@@ -55,7 +54,7 @@ __global__ __launch_bounds__(256) void k_row_planes(PlaneSrc src, _Float16 *__re
     if (threadIdx.x == 0) inv_out[r] = inv;
     for (u32 c = threadIdx.x * 8u; c < Cp; c += 2048u) {
         float v[8];
-        load8<TY>(p + c, wide, c < src.cols ? src.cols - c : 0u, v);
+        load8<TY>(p + c, c < src.cols ? src.cols - c : 0u, v);
         h8 hi, lo;
 #pragma unroll
         for (int i = 0; i < 8; i++) {

@@ -14,22 +14,63 @@ struct RowSum {
 };
 __device__ __forceinline__ RowSum row_sum() { return {-INFINITY, 0.0f}; }
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
-// eight more values; the ones that do not count are -inf.  c: log2 e / T
-__device__ __forceinline__ void add8(RowSum &a, const float (&v)[8], float c)
+// the largest of eight, NaN if one is
+__device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float largest8(const float (&v)[8])
 {
-    float m = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-    m = fmaxf(m, a.m);
-    if (m == -INFINITY) { // (nothing yet, or a NaN, which the sum then keeps)
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (v[i] != v[i]) a.s = v[i];
+    return largest(largest(largest(largest(v[0], v[1]), v[2]), largest(largest(v[3], v[4]), v[5])), largest(v[6], v[7]));
+}
+// eight more values, m8 the largest; the ones that do not count are -inf.  c: log2 e / T
+__device__ __forceinline__ void add8(RowSum &a, const float (&v)[8], float m8, float c)
+{
+    if (m8 > a.m) {
+        a.s *= pow2((a.m - m8) * c);
+        a.m = m8;
+    } else if (a.m == -INFINITY) { // (nothing yet, or a NaN, which the sum then keeps)
+        if (m8 != m8) a.s = m8;
         return;
     }
-    float s = a.s * pow2((a.m - m) * c);
 #pragma unroll
-    for (int i = 0; i < 8; i++) s += pow2((v[i] - m) * c);
-    a.m = m;
-    a.s = s;
+    for (int i = 0; i < 8; i++) a.s += pow2((v[i] - a.m) * c);
+}
+__device__ __forceinline__ void add1(RowSum &a, float x, float c)
+{
+    if (x > a.m) {
+        a.s = a.s * pow2((a.m - x) * c) + 1.0f;
+        a.m = x;
+    } else if (a.m != -INFINITY) {
+        a.s += pow2((x - a.m) * c);
+    }
+}
+
+// A row in steps of eight elements a thread: work(first element, the eight, number of them there) for all of them, four
+// steps asked for at a time.  Steps that are there for every thread are worked on without a look at the row's end.
+template <u32 TY, u32 BLOCK, class F>
+__device__ __forceinline__ void each_step(const GLOBAL_AS typename Elem<TY>::type *p, u32 n, F work)
+{
+    constexpr u32 STEP = BLOCK * 8u;
+    const u32 mine = threadIdx.x * 8u;
+    u32 i0 = 0u;
+    for (; i0 + 4u * STEP <= n; i0 += 4u * STEP) {
+        Raw8<TY> x[4];
+#pragma unroll
+        for (u32 j = 0; j < 4u; j++) x[j] = load_raw8<TY>(p + i0 + j * STEP + mine, 8u);
+#pragma unroll
+        for (u32 j = 0; j < 4u; j++) work(i0 + j * STEP + mine, x[j], 8u, j);
+    }
+    if (i0 < n) {
+        Raw8<TY> x[4];
+#pragma unroll
+        for (u32 j = 0; j < 4u; j++) {
+            const u32 i = i0 + j * STEP + mine;
+            x[j] = load_raw8<TY>(p + i, i < n ? n - i : 0u);
+        }
+#pragma unroll
+        for (u32 j = 0; j < 4u; j++) {
+            const u32 i = i0 + j * STEP + mine;
+            if (i < n) work(i, x[j], min(n - i, 8u), j);
+        }
+    }
 }
 
 __device__ __forceinline__ double wave_sum(double v)
@@ -86,10 +127,25 @@ __device__ __forceinline__ const GLOBAL_AS typename Elem<TY>::type *row_of(const
 // ------------------------------------------------------------------------------------------
 // the largest logits
 // ------------------------------------------------------------------------------------------
-constexpr u32 TOP_BLOCK = 1024, TOP_ROOM = 2048;
+constexpr u32 TOP_ROOM = 2048; // candidates
+constexpr int TOP_MAXIMA = 4;   // a thread keeps the largest of as many parts of its elements (every fourth step)
 
 __device__ __forceinline__ u32 logit_key(float x) { return x != x ? 0xFFFFFFFFu : key_of_float(x); }
 __device__ __forceinline__ float logit_of(u32 key) { return __uint_as_float(bits_of_key(key)); }
+
+// A number that at least k of the wave's keys are not below: the k-th largest, cut to its upper 20 bits.
+__device__ __forceinline__ u32 wave_kth(const u32 (&m)[TOP_MAXIMA], u32 k)
+{
+    u32 t = 0u;
+    for (int b = 31; b >= 12; b--) {
+        const u32 c = t | 1u << b;
+        u32 n = 0u;
+#pragma unroll
+        for (int i = 0; i < TOP_MAXIMA; i++) n += (u32)__popcll(__ballot(m[i] >= c));
+        if (n >= k) t = c;
+    }
+    return t;
+}
 
 template <class T>
 __device__ void sort_descending(T *v, u32 n) // n: a power of two
@@ -109,65 +165,79 @@ __device__ void sort_descending(T *v, u32 n) // n: a power of two
     __syncthreads();
 }
 
-template <u32 TY>
-__global__ __launch_bounds__(TOP_BLOCK) void k_top_logits(LogitsCall c, int *__restrict__ index, float *__restrict__ value, float *__restrict__ tail)
+// The k largest in three steps.  Every wave finds a number that ceil(k / waves) of the largest keys its threads have
+// seen are not below; at least k elements of the row are not below the smallest of these (about 1.2 k for logits in no
+// particular order).  A second reading of the row picks them out and adds the others up.  Each candidate's place is the
+// number of larger ones.
+template <u32 TY, u32 BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restrict__ index, float *__restrict__ value, float *__restrict__ tail)
 {
-    constexpr int WAVES = TOP_BLOCK / 64;
+    constexpr int WAVES = BLOCK / 64;
     __shared__ u64 cand[TOP_ROOM];
-    __shared__ u32 maxima[TOP_BLOCK];
+    __shared__ u32 low[WAVES], counts[WAVES];
     __shared__ double room[WAVES];
     __shared__ u32 n_cand, count;
     const u64 r = blockIdx.x;
     const auto *p = row_of<TY>(c.logits, r);
-    const bool wide = ((u64)p & 15u) == 0u;
     const u32 V = c.n_vocab, k = c.k, tid = threadIdx.x;
     const double inv_T = 1.0 / (double)c.temperature;
     const float c2 = (float)(LOG2E * inv_T);
 
-    // The k-th of the threads' largest keys: at least k elements are not below it.
-    u32 top = 0u;
-    for (u32 i = tid * 8u; i < V; i += TOP_BLOCK * 8u) {
+    float high[TOP_MAXIMA] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    each_step<TY, BLOCK>(p, V, [&](u32, const Raw8<TY> &x, u32 there, u32 j) {
         float v[8];
-        load8<TY>(p + i, wide, V - i, v);
 #pragma unroll
-        for (u32 j = 0; j < 8u; j++)
-            if (i + j < V) top = max(top, logit_key(v[j]));
-    }
-    maxima[tid] = top;
+        for (u32 q = 0; q < 8u; q++) v[q] = q < there ? x[q] : -INFINITY;
+        high[j] = largest(high[j], largest8(v));
+    });
+    u32 top[TOP_MAXIMA];
+#pragma unroll
+    for (int j = 0; j < TOP_MAXIMA; j++) top[j] = logit_key(high[j]);
+    const u32 mine = wave_kth(top, (k + WAVES - 1u) / WAVES);
+    if ((tid & 63u) == 0u) low[tid >> 6] = mine;
     if (tid == 0) n_cand = 0u;
-    sort_descending(maxima, TOP_BLOCK);
-    const u32 thr = maxima[k - 1u], highest = maxima[0];
-
-    // Everything from it on is a candidate; the others are added up.
-    RowSum rest = row_sum();
-    for (u32 i = tid * 8u; i < V; i += TOP_BLOCK * 8u) {
-        float v[8];
-        load8<TY>(p + i, wide, V - i, v);
-#pragma unroll
-        for (u32 j = 0; j < 8u; j++) {
-            const u32 key = logit_key(v[j]);
-            if (i + j >= V) {
-                v[j] = -INFINITY;
-            } else if (key >= thr) {
-                const u32 at = atomicAdd(&n_cand, 1u);
-                if (at < TOP_ROOM) cand[at] = (u64)key << 32 | (u32)~(i + j);
-                v[j] = -INFINITY;
-            }
-        }
-        add8(rest, v, c2);
-    }
     __syncthreads();
+    u32 thr = low[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; w++) thr = min(thr, low[w]);
+
+    const float bound = logit_of(thr); // (NaN where the keys that were cut off it are those of NaN)
+    RowSum rest = row_sum();
+    bool odd = false; // NaN or +inf
+    each_step<TY, BLOCK>(p, V, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
+        float v[8];
+#pragma unroll
+        for (u32 q = 0; q < 8u; q++) v[q] = q < there ? x[q] : -INFINITY;
+        float m8 = largest8(v);
+        if (!(m8 < bound)) {
+#pragma unroll
+            for (u32 q = 0; q < 8u; q++)
+                if (!(v[q] < bound) && q < there) {
+                    odd = odd || !(v[q] < INFINITY);
+                    const u32 at = atomicAdd(&n_cand, 1u);
+                    if (at < TOP_ROOM) cand[at] = (u64)logit_key(v[q]) << 32 | (u32)~(i + q);
+                    v[q] = -INFINITY;
+                }
+            m8 = largest8(v);
+        }
+        add8(rest, v, m8, c2);
+    });
+    odd = __syncthreads_or(odd ? 1 : 0) != 0;
     u32 n = n_cand;
     if (n > TOP_ROOM) {
-        // Too many equal ones: the key of rank k by halving, then the larger ones and the first of the equal ones.
+        // Too many, mostly equal ones: the key of rank k, the larger ones, and the first of the equal ones.  The first
+        // try is whether fewer than k lie above the bound, as in a row with fewer than k allowed logits; then by halving.
         u32 lo = thr, hi = 0xFFFFFFFFu; // count(>= lo) >= k
-        while (lo < hi) {
-            const u32 mid = lo + (hi - lo) / 2u + 1u;
+        for (bool first = true; lo < hi; first = false) {
+            const u32 mid = first ? lo + 1u : lo + (hi - lo) / 2u + 1u;
             __syncthreads();
             if (tid == 0) count = 0u;
             __syncthreads();
             u32 have = 0u;
-            for (u32 i = tid; i < V; i += TOP_BLOCK) have += logit_key(Elem<TY>::get(p[i])) >= mid ? 1u : 0u;
+            each_step<TY, BLOCK>(p, V, [&](u32, const Raw8<TY> &x, u32 there, u32) {
+#pragma unroll
+                for (u32 q = 0; q < 8u; q++) have += q < there && logit_key(x[q]) >= mid ? 1u : 0u;
+            });
             if (have) atomicAdd(&count, have);
             __syncthreads();
             if (count >= k)
@@ -179,69 +249,68 @@ __global__ __launch_bounds__(TOP_BLOCK) void k_top_logits(LogitsCall c, int *__r
         if (tid == 0) n_cand = 0u;
         __syncthreads();
         rest = row_sum();
-        for (u32 i = tid; i < V; i += TOP_BLOCK) {
+        for (u32 i = tid; i < V; i += BLOCK) {
             const float x = Elem<TY>::get(p[i]);
             const u32 key = logit_key(x);
             if (key > lo) cand[atomicAdd(&n_cand, 1u)] = (u64)key << 32 | (u32)~i; // (fewer than k)
-            if (key < lo) {
-                const float one[8] = {x, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                add8(rest, one, c2);
-            }
+            if (key < lo) add1(rest, x, c2);
         }
         __syncthreads();
         n = n_cand;
         u32 equal = 0u; // equal ones before this step of the row, the same in all threads
-        for (u32 i0 = 0; i0 < V; i0 += TOP_BLOCK) {
+        for (u32 i0 = 0; i0 < V; i0 += BLOCK) {
             const u32 i = i0 + tid;
             const bool is = i < V && logit_key(Elem<TY>::get(p[i])) == lo;
             const u64 mask = __ballot(is);
             __syncthreads();
-            if ((tid & 63u) == 0u) maxima[tid >> 6] = (u32)__popcll(mask);
+            if ((tid & 63u) == 0u) counts[tid >> 6] = (u32)__popcll(mask);
             __syncthreads();
-            u32 before = equal, all = 0u;
+            u32 before = equal;
             for (int w = 0; w < WAVES; w++) {
-                if (w < (int)(tid >> 6)) before += maxima[w];
-                all += maxima[w];
+                if (w < (int)(tid >> 6)) before += counts[w];
+                equal += counts[w];
             }
             if (is) {
                 const u32 at = n + before + (u32)__popcll(mask & ((1ull << (tid & 63u)) - 1ull));
                 if (at < k)
                     cand[at] = (u64)lo << 32 | (u32)~i;
-                else if (lo != key_of_float(-INFINITY)) {
-                    const float one[8] = {logit_of(lo), -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    add8(rest, one, c2);
-                }
+                else if (lo != key_of_float(-INFINITY))
+                    add1(rest, logit_of(lo), c2);
             }
-            equal += all;
         }
         __syncthreads();
         n = k;
     }
-    u32 size = 2u;
-    while (size < n) size <<= 1;
-    for (u32 i = n + tid; i < size; i += TOP_BLOCK) cand[i] = 0ull;
-    sort_descending(cand, size);
-    for (u32 i = tid; i < n; i += TOP_BLOCK) {
-        const u32 key = (u32)(cand[i] >> 32);
-        if (i < k) {
-            gptr(index)[r * k + i] = (int)~(u32)cand[i];
-            gptr(value)[r * k + i] = Elem<TY>::get(p[~(u32)cand[i]]);
+    if (n > BLOCK) { // (a place for every thread's candidate: the largest ones first)
+        u32 size = 2u;
+        while (size < n) size <<= 1;
+        for (u32 i = n + tid; i < size; i += BLOCK) cand[i] = 0ull;
+        sort_descending(cand, size);
+        for (u32 i = k + tid; i < n; i += BLOCK) add1(rest, logit_of((u32)(cand[i] >> 32)), c2);
+        n = k;
+    }
+    if (tid < n) {
+        const u64 own = cand[tid];
+        u32 place = 0u;
+        for (u32 i = 0; i < n; i++) place += cand[i] > own ? 1u : 0u;
+        const u32 at = (u32)~(u32)own;
+        if (place < k) {
+            gptr(index)[r * k + place] = (int)at;
+            gptr(value)[r * k + place] = Elem<TY>::get(p[at]); // (of the two zeros the one that is there)
         } else {
-            const float one[8] = {logit_of(key), -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            add8(rest, one, c2);
+            add1(rest, logit_of((u32)(own >> 32)), c2);
         }
     }
     if (tail) {
         const double l = block_log<WAVES>(rest, inv_T, room);
-        if (tid == 0) gptr(tail)[r] = highest >= key_of_float(INFINITY) ? __uint_as_float(0x7fc00000u) : (float)l;
+        if (tid == 0) gptr(tail)[r] = odd ? __uint_as_float(0x7fc00000u) : (float)l;
     }
 }
 
 // ------------------------------------------------------------------------------------------
 // the loss
 // ------------------------------------------------------------------------------------------
-constexpr u32 DIST_BLOCK = 256; // threads; at least MAX_LISTED
-static_assert(DIST_BLOCK >= MAX_LISTED, "a thread per listed entry");
+static_assert(MAX_LISTED <= 256, "a thread per listed entry");
 // Saved per row: log of the student's sum, log of its part that is not listed, log of the teacher's sum, and what the
 // unlisted ones' gradient is of their share of that part: q - P_tail e^(u - log_out) = e^(u - log_out) (q_rest - P_tail).
 constexpr int SAVED = 4;
@@ -261,33 +330,35 @@ __device__ __forceinline__ int listed_entry(const LogitsCall &c, u64 r, int *idx
     return i;
 }
 
-template <u32 TY>
-__global__ __launch_bounds__(DIST_BLOCK) void k_distill(LogitsCall c, float *__restrict__ loss, double *__restrict__ saved)
+template <u32 TY, u32 BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restrict__ loss, double *__restrict__ saved)
 {
-    constexpr int WAVES = DIST_BLOCK / 64;
+    constexpr int WAVES = BLOCK / 64;
     extern __shared__ u32 bits[]; // which logits are listed
     __shared__ int idx[MAX_LISTED];
     __shared__ double room[WAVES];
     const u64 r = blockIdx.x;
     const auto *p = row_of<TY>(c.logits, r);
-    const bool wide = ((u64)p & 15u) == 0u;
     const u32 V = c.n_vocab, tid = threadIdx.x;
     const double inv_T = 1.0 / (double)c.temperature;
     const float c2 = (float)(LOG2E * inv_T);
-    for (u32 i = tid; i < (V + 31u) / 32u; i += DIST_BLOCK) bits[i] = 0u;
+    for (u32 i = tid; i < (V + 31u) / 32u; i += BLOCK) bits[i] = 0u;
     const int mine = listed_entry(c, r, idx); // (a barrier inside)
     if (mine >= 0) atomicOr(&bits[mine >> 5], 1u << (mine & 31));
     __syncthreads();
     RowSum rest = row_sum();
-    for (u32 i = tid * 8u; i < V; i += DIST_BLOCK * 8u) {
-        float v[8];
-        load8<TY>(p + i, wide, V - i, v);
+    each_step<TY, BLOCK>(p, V, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
         const u32 b = ((const unsigned char *)bits)[i >> 3];
+        float v[8];
 #pragma unroll
-        for (u32 j = 0; j < 8u; j++)
-            if (i + j >= V || (b >> j & 1u)) v[j] = -INFINITY;
-        add8(rest, v, c2);
-    }
+        for (u32 q = 0; q < 8u; q++) v[q] = q < there ? x[q] : -INFINITY;
+        if (b) {
+#pragma unroll
+            for (u32 q = 0; q < 8u; q++)
+                if (b >> q & 1u) v[q] = -INFINITY;
+        }
+        add8(rest, v, largest8(v), c2);
+    });
     const double log_out = block_log<WAVES>(rest, inv_T, room);
     // the listed ones, and the teacher's, in fp64: the loss is a small difference of logarithms
     const double t = mine >= 0 ? (double)gptr(c.value)[r * c.k + tid] * inv_T : -INFINITY;
@@ -325,15 +396,14 @@ __global__ __launch_bounds__(DIST_BLOCK) void k_distill(LogitsCall c, float *__r
     }
 }
 
-template <u32 TY>
-__global__ __launch_bounds__(DIST_BLOCK) void k_distill_grad(LogitsCall c, const double *__restrict__ saved, const float *__restrict__ g, Mat grad)
+template <u32 TY, u32 BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const double *__restrict__ saved, const float *__restrict__ g, Mat grad)
 {
     typedef typename Elem<TY>::type T;
     __shared__ int idx[MAX_LISTED];
     const u64 r = blockIdx.x;
     const auto *p = row_of<TY>(c.logits, r);
     GLOBAL_AS T *out = (GLOBAL_AS T *)grad.p + r * grad.stride;
-    const bool wide = (((u64)p | (u64)out) & 15u) == 0u;
     const u32 V = c.n_vocab, tid = threadIdx.x;
     const double inv_T = 1.0 / (double)c.temperature;
     const double log_s = gptr(saved)[r * SAVED + 0];
@@ -351,24 +421,23 @@ __global__ __launch_bounds__(DIST_BLOCK) void k_distill_grad(LogitsCall c, const
     // e^(z / T - log_out) = 2^(z c - l), c and l in two parts each
     const double c64 = LOG2E * inv_T, l64 = empty ? 0.0 : gptr(saved)[r * SAVED + 1] * LOG2E;
     const float ch = (float)c64, cl = (float)(c64 - (double)ch), lh = (float)l64, ll = (float)(l64 - (double)lh);
-    for (u32 i = tid * 8u; i < V; i += DIST_BLOCK * 8u) {
-        float v[8];
-        load8<TY>(p + i, wide, V - i, v);
+    // (two steps ahead are asked for before one is worked on; a step's own elements are read before they are written)
+    constexpr u32 STEP = BLOCK * 8u;
+    const u32 first = tid * 8u;
+    Raw8<TY> ahead[2];
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = empty || v[j] == -INFINITY ? 0.0f : f * pow2(fmaf(v[j], ch, -lh) + fmaf(v[j], cl, -ll));
-        if (wide && V - i >= 8u) {
-            union {
-                u4_16 q[sizeof(T) / 2];
-                T e[8];
-            } x;
+    for (u32 j = 0; j < 2u; j++) ahead[j] = load_raw8<TY>(p + first + j * STEP, first + j * STEP < V ? V - first - j * STEP : 0u);
+    for (u32 i0 = 0; i0 < V; i0 += 2u * STEP) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) x.e[j] = Elem<TY>::put(v[j]);
+        for (u32 j = 0; j < 2u; j++) {
+            const u32 i = i0 + j * STEP + first, next = i + 2u * STEP;
+            const Raw8<TY> x = ahead[j];
+            ahead[j] = load_raw8<TY>(p + next, next < V ? V - next : 0u);
+            if (i >= V) continue;
+            float v[8];
 #pragma unroll
-            for (u32 j = 0; j < sizeof(T) / 2; j++) ((GLOBAL_AS u4_16 *)(out + i))[j] = x.q[j];
-        } else {
-#pragma unroll
-            for (u32 j = 0; j < 8u; j++)
-                if (i + j < V) out[i + j] = Elem<TY>::put(v[j]);
+            for (int q = 0; q < 8; q++) v[q] = empty || x[q] == -INFINITY ? 0.0f : f * pow2(fmaf(x[q], ch, -lh) + fmaf(x[q], cl, -ll));
+            store8<TY>(out + i, V - i, v);
         }
     }
     __syncthreads();
@@ -378,33 +447,58 @@ __global__ __launch_bounds__(DIST_BLOCK) void k_distill_grad(LogitsCall c, const
 // ------------------------------------------------------------------------------------------
 // calls
 // ------------------------------------------------------------------------------------------
+namespace {
+
+// A workgroup per row: 256 threads where the rows fill the chip (eight workgroups a CU), 1024 where there are few, each of
+// which is then read in fewer steps.
+constexpr u64 FEW_ROWS = 512;
+
+template <u32 TY, u32 BLOCK>
+void start_top(const LogitsCall &c, int *index, float *value, float *tail, hipStream_t s)
+{
+    PROF("k_top_logits", s, k_top_logits<TY, BLOCK><<<(u32)c.rows, BLOCK, 0, s>>>(c, index, value, tail));
+}
+template <u32 TY, u32 BLOCK>
+void start_distill(const LogitsCall &c, float *loss, double *saved, hipStream_t s)
+{
+    PROF("k_distill", s, k_distill<TY, BLOCK><<<(u32)c.rows, BLOCK, (c.n_vocab + 31u) / 32u * 4u, s>>>(c, loss, saved));
+}
+template <u32 TY, u32 BLOCK>
+void start_grad(const LogitsCall &c, const double *saved, const float *g, const Mat &grad, hipStream_t s)
+{
+    PROF("k_distill_grad", s, k_distill_grad<TY, BLOCK><<<(u32)c.rows, BLOCK, 0, s>>>(c, saved, g, grad));
+}
+
+} // namespace
+
 hipError_t launch_top_logits(const LogitsCall &c, int *index, float *value, float *tail, hipStream_t s)
 {
-    const u32 grid = (u32)c.rows;
+    // (k of 1024 threads' maxima: every wave has to have seen k / 16 elements' worth of them)
+    const bool few = c.rows < FEW_ROWS && c.n_vocab >= 8192u;
     switch (c.type) {
-    case TY_F32: PROF("k_top_logits", s, k_top_logits<TY_F32><<<grid, TOP_BLOCK, 0, s>>>(c, index, value, tail)); break;
-    case TY_BF16: PROF("k_top_logits", s, k_top_logits<TY_BF16><<<grid, TOP_BLOCK, 0, s>>>(c, index, value, tail)); break;
-    default: PROF("k_top_logits", s, k_top_logits<TY_F16><<<grid, TOP_BLOCK, 0, s>>>(c, index, value, tail)); break;
+    case TY_F32: few ? start_top<TY_F32, 1024>(c, index, value, tail, s) : start_top<TY_F32, 256>(c, index, value, tail, s); break;
+    case TY_BF16: few ? start_top<TY_BF16, 1024>(c, index, value, tail, s) : start_top<TY_BF16, 256>(c, index, value, tail, s); break;
+    default: few ? start_top<TY_F16, 1024>(c, index, value, tail, s) : start_top<TY_F16, 256>(c, index, value, tail, s); break;
     }
     return hipGetLastError();
 }
 hipError_t launch_distill(const LogitsCall &c, float *loss, double *saved, hipStream_t s)
 {
-    const u32 grid = (u32)c.rows, lds = (c.n_vocab + 31u) / 32u * 4u;
+    const bool few = c.rows < FEW_ROWS;
     switch (c.type) {
-    case TY_F32: PROF("k_distill", s, k_distill<TY_F32><<<grid, DIST_BLOCK, lds, s>>>(c, loss, saved)); break;
-    case TY_BF16: PROF("k_distill", s, k_distill<TY_BF16><<<grid, DIST_BLOCK, lds, s>>>(c, loss, saved)); break;
-    default: PROF("k_distill", s, k_distill<TY_F16><<<grid, DIST_BLOCK, lds, s>>>(c, loss, saved)); break;
+    case TY_F32: few ? start_distill<TY_F32, 1024>(c, loss, saved, s) : start_distill<TY_F32, 256>(c, loss, saved, s); break;
+    case TY_BF16: few ? start_distill<TY_BF16, 1024>(c, loss, saved, s) : start_distill<TY_BF16, 256>(c, loss, saved, s); break;
+    default: few ? start_distill<TY_F16, 1024>(c, loss, saved, s) : start_distill<TY_F16, 256>(c, loss, saved, s); break;
     }
     return hipGetLastError();
 }
 hipError_t launch_distill_grad(const LogitsCall &c, const double *saved, const float *g, const Mat &grad, hipStream_t s)
 {
-    const u32 grid = (u32)c.rows;
+    const bool few = c.rows < FEW_ROWS;
     switch (c.type) {
-    case TY_F32: PROF("k_distill_grad", s, k_distill_grad<TY_F32><<<grid, DIST_BLOCK, 0, s>>>(c, saved, g, grad)); break;
-    case TY_BF16: PROF("k_distill_grad", s, k_distill_grad<TY_BF16><<<grid, DIST_BLOCK, 0, s>>>(c, saved, g, grad)); break;
-    default: PROF("k_distill_grad", s, k_distill_grad<TY_F16><<<grid, DIST_BLOCK, 0, s>>>(c, saved, g, grad)); break;
+    case TY_F32: few ? start_grad<TY_F32, 1024>(c, saved, g, grad, s) : start_grad<TY_F32, 256>(c, saved, g, grad, s); break;
+    case TY_BF16: few ? start_grad<TY_BF16, 1024>(c, saved, g, grad, s) : start_grad<TY_BF16, 256>(c, saved, g, grad, s); break;
+    default: few ? start_grad<TY_F16, 1024>(c, saved, g, grad, s) : start_grad<TY_F16, 256>(c, saved, g, grad, s); break;
     }
     return hipGetLastError();
 }
