@@ -85,36 +85,31 @@ __device__ __forceinline__ double wave_max(double v)
     for (int d = 32; d; d >>= 1) v = fmax(v, __shfl_xor(v, d));
     return v;
 }
-// Over all threads of the workgroup, the same for everybody; `room`: a double per wave.
-template <int WAVES>
-__device__ double block_sum(double v, double *room)
+// What the threads' sums are together, for every wave to join from `room` (a place per wave) after a barrier.
+__device__ __forceinline__ void put_sum(const RowSum &a, double c, double2 *room)
 {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63u) == 0u) room[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.0;
-    for (int i = 0; i < WAVES; i++) v += room[i];
-    return v;
+    float m = a.m;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    double s = a.m == m && a.s == a.s ? (double)a.s : a.s > 0.0f ? (double)a.s * exp2(((double)a.m - (double)m) * c) : a.s != a.s ? (double)a.s : 0.0;
+    s = wave_sum(s);
+    if ((threadIdx.x & 63u) == 0u) room[threadIdx.x >> 6] = make_double2((double)m, s);
 }
+// The logarithm of the whole sum, -inf where nothing counts; by all lanes of a wave.
 template <int WAVES>
-__device__ double block_max(double v, double *room)
+__device__ __forceinline__ double joined_log(const double2 *room, double inv_T)
 {
-    v = wave_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 63u) == 0u) room[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = room[0];
-    for (int i = 1; i < WAVES; i++) v = fmax(v, room[i]);
-    return v;
-}
-// log of the sum that the threads hold together, -inf where nothing counts
-template <int WAVES>
-__device__ double block_log(const RowSum &a, double inv_T, double *room)
-{
-    const double m = block_max<WAVES>((double)a.m, room);
-    const double part = a.s > 0.0f ? (double)a.s * exp(((double)a.m - m) * inv_T) : (a.s != a.s ? (double)a.s : 0.0);
-    const double s = block_sum<WAVES>(part, room);
+    const u32 lane = threadIdx.x & 63u;
+    double2 v = make_double2(-INFINITY, 0.0);
+    if (lane < (u32)WAVES) v = room[lane];
+    double m = v.x;
+#pragma unroll
+    for (int d = 8; d; d >>= 1) m = fmax(m, __shfl_xor(m, d)); // (up to 16 waves)
+    double s = v.y > 0.0 ? v.y * exp((v.x - m) * inv_T) : v.y;
+#pragma unroll
+    for (int d = 8; d; d >>= 1) s += __shfl_xor(s, d);
+    m = __shfl(m, 0);
+    s = __shfl(s, 0);
     return s > 0.0 ? m * inv_T + log(s) : s != s ? s : -INFINITY;
 }
 
@@ -175,7 +170,7 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
     constexpr int WAVES = BLOCK / 64;
     __shared__ u64 cand[TOP_ROOM];
     __shared__ u32 low[WAVES], counts[WAVES];
-    __shared__ double room[WAVES];
+    __shared__ double2 room[WAVES];
     __shared__ u32 n_cand, count;
     const u64 r = blockIdx.x;
     const auto *p = row_of<TY>(c.logits, r);
@@ -292,6 +287,7 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
     if (tid < n) {
         const u64 own = cand[tid];
         u32 place = 0u;
+#pragma unroll 8
         for (u32 i = 0; i < n; i++) place += cand[i] > own ? 1u : 0u;
         const u32 at = (u32)~(u32)own;
         if (place < k) {
@@ -302,7 +298,10 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
         }
     }
     if (tail) {
-        const double l = block_log<WAVES>(rest, inv_T, room);
+        put_sum(rest, LOG2E * inv_T, room);
+        __syncthreads();
+        if (tid >= 64u) return;
+        const double l = joined_log<WAVES>(room, inv_T);
         if (tid == 0) gptr(tail)[r] = odd ? __uint_as_float(0x7fc00000u) : (float)l;
     }
 }
@@ -315,36 +314,45 @@ static_assert(MAX_LISTED <= 256, "a thread per listed entry");
 // unlisted ones' gradient is of their share of that part: q - P_tail e^(u - log_out) = e^(u - log_out) (q_rest - P_tail).
 constexpr int SAVED = 4;
 
-// This thread's entry of the list, or -1: no thread, no index of the vocabulary, or one that stands earlier in the list.
-__device__ __forceinline__ int listed_entry(const LogitsCall &c, u64 r, int *idx)
+// Entry j of the row's list into idx[j], -1 for an index outside the vocabulary; idx has room for MAX_LISTED and is -1
+// past the list.  A barrier has to follow.
+__device__ __forceinline__ void read_list(const LogitsCall &c, u64 r, int *idx)
 {
-    int i = -1;
-    if (threadIdx.x < c.k) {
-        i = gptr(c.index)[r * c.k + threadIdx.x];
-        if (i < 0 || (u32)i >= c.n_vocab) i = -1;
-        idx[threadIdx.x] = i;
+    for (u32 j = threadIdx.x; j < MAX_LISTED; j += blockDim.x) {
+        const int i = j < c.k ? gptr(c.index)[r * c.k + j] : -1;
+        idx[j] = (u32)i < c.n_vocab ? i : -1;
     }
-    __syncthreads();
-    for (u32 j = 0; j < threadIdx.x && j < c.k; j++)
-        if (idx[j] == i) i = -1;
-    return i;
+}
+// Entry j, or -1 where its index stands earlier in the list.
+__device__ __forceinline__ int first_of(const int *idx, u32 j)
+{
+    const int i = idx[j];
+    const int4 *four = (const int4 *)idx;
+    bool again = false;
+    for (u32 q = 0; 4u * q < j; q++) {
+        const int4 v = four[q];
+        again = again || v.x == i || (v.y == i && 4u * q + 1u < j) || (v.z == i && 4u * q + 2u < j) || (v.w == i && 4u * q + 3u < j);
+    }
+    return again ? -1 : i;
 }
 
+// The first wave ends the row: 64 lanes with up to four listed entries each.
 template <u32 TY, u32 BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restrict__ loss, double *__restrict__ saved)
 {
     constexpr int WAVES = BLOCK / 64;
     extern __shared__ u32 bits[]; // which logits are listed
-    __shared__ int idx[MAX_LISTED];
-    __shared__ double room[WAVES];
+    __shared__ __attribute__((aligned(16))) int idx[MAX_LISTED];
+    __shared__ double2 room[WAVES];
     const u64 r = blockIdx.x;
     const auto *p = row_of<TY>(c.logits, r);
     const u32 V = c.n_vocab, tid = threadIdx.x;
     const double inv_T = 1.0 / (double)c.temperature;
     const float c2 = (float)(LOG2E * inv_T);
     for (u32 i = tid; i < (V + 31u) / 32u; i += BLOCK) bits[i] = 0u;
-    const int mine = listed_entry(c, r, idx); // (a barrier inside)
-    if (mine >= 0) atomicOr(&bits[mine >> 5], 1u << (mine & 31));
+    read_list(c, r, idx);
+    __syncthreads();
+    if (tid < c.k && idx[tid] >= 0) atomicOr(&bits[idx[tid] >> 5], 1u << (idx[tid] & 31));
     __syncthreads();
     RowSum rest = row_sum();
     each_step<TY, BLOCK>(p, V, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
@@ -359,26 +367,53 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
         }
         add8(rest, v, largest8(v), c2);
     });
-    const double log_out = block_log<WAVES>(rest, inv_T, room);
+    put_sum(rest, LOG2E * inv_T, room);
+    __syncthreads();
+    if (tid >= 64u) return;
     // the listed ones, and the teacher's, in fp64: the loss is a small difference of logarithms
-    const double t = mine >= 0 ? (double)gptr(c.value)[r * c.k + tid] * inv_T : -INFINITY;
-    const double u = mine >= 0 ? (double)Elem<TY>::get(p[mine]) * inv_T : -INFINITY;
-    const double tail = c.tail ? (double)gptr(c.tail)[r] : -INFINITY;
-    const double mt = fmax(block_max<WAVES>(t, room), tail), ms = fmax(block_max<WAVES>(u, room), log_out);
-    const double any = block_sum<WAVES>(mine >= 0 ? 1.0 : 0.0, room);
-    const double st = block_sum<WAVES>(t == -INFINITY ? 0.0 : exp(t - mt), room);
-    const double ss = block_sum<WAVES>(u == -INFINITY ? 0.0 : exp(u - ms), room);
+    double t[4], u[4], tail = c.tail ? (double)gptr(c.tail)[r] : -INFINITY, mt = tail, ms = -INFINITY;
+    bool any = false;
+#pragma unroll
+    for (u32 q = 0; q < 4u; q++) {
+        t[q] = u[q] = -INFINITY;
+        if (64u * q >= c.k) continue; // (the same for all lanes)
+        const int i = first_of(idx, tid + 64u * q);
+        if (i < 0) continue;
+        any = true;
+        t[q] = (double)gptr(c.value)[r * c.k + tid + 64u * q] * inv_T;
+        u[q] = (double)Elem<TY>::get(p[i]) * inv_T;
+        mt = t[q] != t[q] ? t[q] : fmax(mt, t[q]);
+        ms = fmax(ms, u[q]);
+    }
+    const double log_out = joined_log<WAVES>(room, inv_T);
+    any = __ballot(any) != 0;
+    mt = wave_max(mt);
+    ms = fmax(wave_max(ms), log_out);
+    double st = 0.0, ss = 0.0;
+#pragma unroll
+    for (u32 q = 0; q < 4u; q++) {
+        if (64u * q >= c.k) continue;
+        if (t[q] != -INFINITY) st += exp(t[q] - mt);
+        if (u[q] != -INFINITY) ss += exp(u[q] - ms);
+    }
+    st = wave_sum(st);
+    ss = wave_sum(ss);
     const double log_t = mt + log(st + (tail == -INFINITY ? 0.0 : exp(tail - mt)));
     const double log_s = ms + log(ss + (log_out == -INFINITY ? 0.0 : exp(log_out - ms)));
-    const bool empty = any == 0.0 || mt == -INFINITY || ms == -INFINITY;
+    const bool empty = !any || mt == -INFINITY || ms == -INFINITY;
     // sum P (e^d - 1 - d), d = log q - log P: as the listed ones and the rest add up to 1 on both sides, errors of the two
     // logarithms of sums cancel to first order
-    double one = 0.0;
-    if (mine >= 0 && !empty) {
-        const double lp = t - log_t, d = (u - log_s) - lp;
-        one = t == -INFINITY ? exp(u - log_s) : exp(lp) * (expm1(d) - d);
+    double all = 0.0;
+#pragma unroll
+    for (u32 q = 0; q < 4u; q++) {
+        if (64u * q >= c.k || empty) continue;
+        const double lp = t[q] - log_t, d = (u[q] - log_s) - lp;
+        if (t[q] != -INFINITY)
+            all += exp(lp) * (expm1(d) - d);
+        else if (u[q] != -INFINITY)
+            all += exp(u[q] - log_s);
     }
-    double all = block_sum<WAVES>(one, room);
+    all = wave_sum(all);
     if (tid == 0) {
         double over = 0.0;
         if (!empty) {
@@ -400,7 +435,7 @@ template <u32 TY, u32 BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const double *__restrict__ saved, const float *__restrict__ g, Mat grad)
 {
     typedef typename Elem<TY>::type T;
-    __shared__ int idx[MAX_LISTED];
+    __shared__ __attribute__((aligned(16))) int idx[MAX_LISTED];
     const u64 r = blockIdx.x;
     const auto *p = row_of<TY>(c.logits, r);
     GLOBAL_AS T *out = (GLOBAL_AS T *)grad.p + r * grad.stride;
@@ -409,7 +444,9 @@ __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const doub
     const double log_s = gptr(saved)[r * SAVED + 0];
     const bool empty = log_s == INFINITY;
     const double up = (g ? (double)gptr(g)[r] : 1.0) * inv_T;
-    const int mine = listed_entry(c, r, idx);
+    read_list(c, r, idx);
+    __syncthreads();
+    const int mine = tid < c.k ? first_of(idx, tid) : -1;
     float at_mine = 0.0f;
     if (mine >= 0 && !empty) {
         const double t = (double)gptr(c.value)[r * c.k + tid] * inv_T;
@@ -421,25 +458,16 @@ __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const doub
     // e^(z / T - log_out) = 2^(z c - l), c and l in two parts each
     const double c64 = LOG2E * inv_T, l64 = empty ? 0.0 : gptr(saved)[r * SAVED + 1] * LOG2E;
     const float ch = (float)c64, cl = (float)(c64 - (double)ch), lh = (float)l64, ll = (float)(l64 - (double)lh);
-    // (two steps ahead are asked for before one is worked on; a step's own elements are read before they are written)
-    constexpr u32 STEP = BLOCK * 8u;
-    const u32 first = tid * 8u;
-    Raw8<TY> ahead[2];
+    auto slope = [&](float x) { return empty || x == -INFINITY ? 0.0f : f * pow2(fmaf(x, ch, -lh) + fmaf(x, cl, -ll)); };
+    // The steps begin where the results' lines of 128 bytes begin; an element of a step is read before it is written.
+    const u32 head = min((u32)((0ull - (u64)out) & 127ull) / (u32)sizeof(T), V);
+    if (tid < head) out[tid] = Elem<TY>::put(slope(Elem<TY>::get(p[tid])));
+    each_step<TY, BLOCK>(p + head, V - head, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
+        float v[8];
 #pragma unroll
-    for (u32 j = 0; j < 2u; j++) ahead[j] = load_raw8<TY>(p + first + j * STEP, first + j * STEP < V ? V - first - j * STEP : 0u);
-    for (u32 i0 = 0; i0 < V; i0 += 2u * STEP) {
-#pragma unroll
-        for (u32 j = 0; j < 2u; j++) {
-            const u32 i = i0 + j * STEP + first, next = i + 2u * STEP;
-            const Raw8<TY> x = ahead[j];
-            ahead[j] = load_raw8<TY>(p + next, next < V ? V - next : 0u);
-            if (i >= V) continue;
-            float v[8];
-#pragma unroll
-            for (int q = 0; q < 8; q++) v[q] = empty || x[q] == -INFINITY ? 0.0f : f * pow2(fmaf(x[q], ch, -lh) + fmaf(x[q], cl, -ll));
-            store8<TY>(out + i, V - i, v);
-        }
-    }
+        for (int q = 0; q < 8; q++) v[q] = slope(x[q]);
+        store8<TY>(out + head + i, there, v);
+    });
     __syncthreads();
     if (mine >= 0) out[mine] = Elem<TY>::put(at_mine);
 }
