@@ -279,16 +279,16 @@ __device__ void finish(const Few &f, char *lds, u64 lo, u64 hi, u32 m0, u32 n0, 
             __syncthreads();
         }
     }
-    for (u32 i = threadIdx.x; i < cells / 4u; i += blockDim.x) {
-        const u32 m = i / (f.cols / 4u), n = (i - m * (f.cols / 4u)) * 4u;
+    for (u32 i = threadIdx.x; i < cells / 8u; i += blockDim.x) {
+        const u32 m = i / (f.cols / 8u), n = (i - m * (f.cols / 8u)) * 8u;
         if (n0 + n >= f.n_out) continue;
-        f4 v;
+        float v[8];
 #pragma unroll
-        for (u32 t = 0; t < 4u; t++) {
+        for (u32 t = 0; t < 8u; t++) {
             v[t] = sums[m * f.cols + n + t] * inv;
             if (any) v[t] += (float)ldexp((double)(long long)listed[m * f.cols + n + t], (int)(high[m] >> 23) - 166);
         }
-        epilogue4<TY>(f.end, m0 + m, n0 + n, v);
+        finish8<TY>(f.end, m0 + m, n0 + n, v);
     }
 }
 

@@ -11,13 +11,14 @@
 // (three planes of bfloat16 would need six passes for fp32, and two for bfloat16 results).
 #include "inshr_product.h"
 
+#include <algorithm>
+
 namespace inshr {
 
 // ------------------------------------------------------------------------------------------
 // planes of an operand whose reduction runs along its rows
 // ------------------------------------------------------------------------------------------
 constexpr u32 KT = 64;  // reduction per step of the product: planes are padded to it with zeros
-constexpr u32 RT = 128; // rows and columns of a workgroup's tile
 inline u64 up(u64 v, u64 to) { return (v + to - 1) / to * to; }
 
 struct PlaneSrc { // a matrix of elements; act != ACT_NONE: multiplied by the slope at the values of `pre`
@@ -236,74 +237,154 @@ struct Gemm {
     const _Float16 *a, *b;   // planes [M][ld], [N][ld]
     u64 plane_a, plane_b;
     u32 M, N, ld;            // ld: the padded reduction, of both
-    u32 n_tiles;             // along N
+    u32 n_tiles, m_tiles;
     u32 pairs;               // number of passes
     u32 pa, pb;              // plane of pass i: bit i
     const float *inv_a, *inv_b; // per row; inv_b NULL: the weight's
     const u32 *wpart;
     Finish end;
     u32 type;                // of the results
+    u32 splits, steps;       // the reduction is dealt to `splits` workgroups, `steps` steps of KT each
+    float *partial;          // [splits][M][n8] their sums; NULL: one workgroup has the whole reduction
+    u32 n8;                  // N rounded up to 8
 };
 
-template <u32 TY>
-__global__ __launch_bounds__(256) void k_product(Gemm g)
+// 16 bytes per lane from device memory to LDS without registers in between: lane l's go to `to` + 16 l.
+__device__ __forceinline__ void to_lds(const _Float16 *from, _Float16 *to)
 {
-    constexpr u32 LD = KT + 8;
-    __shared__ _Float16 As[RT * LD], Bs[RT * LD];
-    const u32 m0 = blockIdx.x / g.n_tiles * RT, n0 = blockIdx.x % g.n_tiles * RT;
+    __builtin_amdgcn_global_load_lds((const GLOBAL_AS u32 *)from, (LDS_AS u32 *)to, 16, 0, 0);
+}
+
+// The scaled sums of row m, columns n .. n + 7, to where they belong.
+template <u32 TY>
+__device__ __forceinline__ void scaled8(const Gemm &g, u32 m, u32 n, float (&v)[8], float inv_w)
+{
+    const float inv_a = gptr(g.inv_a)[m];
+    float b[8];
+    if (g.inv_b) load8<TY_F32>(gptr(g.inv_b) + n, min(g.N - n, 8u), b);
+#pragma unroll
+    for (int t = 0; t < 8; t++) v[t] = v[t] * inv_a * (g.inv_b ? b[t] : inv_w);
+    finish8<TY>(g.end, m, n, v);
+}
+
+// A tile of BM x BN, by waves of WM x WN.  A step takes 64 of the reduction: rows of 128 bytes in LDS, whose eight pieces
+// of 16 bytes lie in an order of the row's own (piece c at c ^ (row / 2 % 8)), so that the 16 rows that a read touches
+// fall into different banks.  The next step's rows are on their way while one is worked on.
+template <u32 TY, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
+{
+    constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TM = WM / 16, TN = WN / 16;
+    constexpr int LOADS = (BM + BN) / 8 / WAVES; // of 8 rows each, per wave and step
+    __shared__ __attribute__((aligned(1024))) _Float16 lds[2][(BM + BN) * KT];
     const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
-    const u32 wm = (wave & 1u) * 64u, wn = (wave >> 1) * 64u;
-    f4 acc[4][4] = {};
-    for (u32 k0 = 0; k0 < g.ld; k0 += KT)
-        for (u32 p = 0; p < g.pairs; p++) {
-            const _Float16 *a = g.a + ((g.pa >> p) & 1u) * g.plane_a, *b = g.b + ((g.pb >> p) & 1u) * g.plane_b;
-            h8 va[4], vb[4];
+    // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles whose rows it finds in its own L2.
+    u32 id = blockIdx.x;
+    const u32 tiles = g.m_tiles * g.n_tiles, split = id / tiles;
+    id -= split * tiles;
+    const u32 per = (tiles + 7u) / 8u, full = tiles - (per - 1u) * 8u; // the first `full` XCDs have `per` tiles
+    const u32 xcd = id & 7u, at = id >> 3;
+    id = xcd < full ? xcd * per + at : full * per + (xcd - full) * (per - 1u) + at;
+    const u32 m0 = id % g.m_tiles * BM, n0 = id / g.m_tiles * BN;
+    const u32 wm = wave % WAVES_M * WM, wn = wave / WAVES_M * WN;
+    // this lane's pieces of a step: row r of the tile's rows (a's, then b's)
+    u64 from[LOADS];
+    bool is_b[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; j++) {
+        const u32 r = (wave * LOADS + j) * 8u + (lane >> 3), c = (lane & 7u) ^ ((r >> 1) & 7u);
+        is_b[j] = (wave * LOADS + j) * 8u >= (u32)BM;
+        // (rows past the last are the last: their results are not stored)
+        const u32 row = is_b[j] ? min(n0 + r - BM, g.N - 1u) : min(m0 + r, g.M - 1u);
+        from[j] = (u64)row * g.ld + c * 8u;
+    }
+    const u32 step0 = split * g.steps, n_steps = min(g.steps, g.ld / KT - step0) * g.pairs;
+    u32 k = step0 * KT, pass = 0;
+    auto fetch = [&](int buf) {
+        const _Float16 *a = g.a + ((g.pa >> pass) & 1u) * g.plane_a + k, *b = g.b + ((g.pb >> pass) & 1u) * g.plane_b + k;
+#pragma unroll
+        for (int j = 0; j < LOADS; j++) to_lds((is_b[j] ? b : a) + from[j], lds[buf] + (wave * LOADS + j) * 8u * KT);
+        if (++pass == g.pairs) {
+            pass = 0;
+            k += KT;
+        }
+    };
+    f4 acc[TM][TN] = {};
+    fetch(0);
+    for (u32 t = 0; t < n_steps; t++) {
+        __syncthreads(); // this step's rows have come, and the other buffer has been read
+        if (t + 1 < n_steps) fetch((t + 1) & 1);
+        const _Float16 *as = lds[t & 1], *bs = as + BM * KT;
+#pragma unroll
+        for (u32 kk = 0; kk < 2u; kk++) {
+            h8 fa[TM], fb[TN];
+            const u32 r = lane & 15u, c = ((kk * 4u + (lane >> 4)) ^ (r >> 1)) * 8u;
+#pragma unroll
+            for (u32 i = 0; i < TM; i++) fa[i] = *(const h8 *)(as + (wm + i * 16u + r) * KT + c);
+#pragma unroll
+            for (u32 j = 0; j < TN; j++) fb[j] = *(const h8 *)(bs + (wn + j * 16u + r) * KT + c);
+            // (the columns of C are the rows of the instruction's result: a lane gets four consecutive ones)
+#pragma unroll
+            for (u32 i = 0; i < TM; i++)
+#pragma unroll
+                for (u32 j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        }
+    }
+    // The sums go through LDS, 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
+    static_assert(WM % 64 == 0 && WN == 64, "");
+    float s, inv_w = 1.0f;
+    if (!g.inv_b && !g.partial) weight_scale(g.wpart, s, inv_w);
+    float *const mine = (float *)lds + wave * 4096u; // [64][64], the pieces of 4 of a row in an order of its own
+#pragma unroll
+    for (int half = 0; half < WM / 64; half++) {
+        __syncthreads();
+#pragma unroll
+        for (u32 i = 0; i < 4u; i++)
 #pragma unroll
             for (u32 j = 0; j < 4u; j++) {
-                const u32 i = threadIdx.x + 256u * j, r = i >> 3, c = (i & 7u) * 8u;
-                // (rows past the last are the last: their results are not stored)
-                va[j] = *(const h8 *)(a + (u64)min(m0 + r, g.M - 1u) * g.ld + k0 + c);
-                vb[j] = *(const h8 *)(b + (u64)min(n0 + r, g.N - 1u) * g.ld + k0 + c);
+                const u32 r = lane & 15u, c = j * 4u + (lane >> 4);
+                *(f4 *)(mine + (i * 16u + r) * 64u + ((c ^ r) * 4u)) = acc[half * 4 + i][j];
             }
-            __syncthreads();
-#pragma unroll
-            for (u32 j = 0; j < 4u; j++) {
-                const u32 i = threadIdx.x + 256u * j, r = i >> 3, c = (i & 7u) * 8u;
-                *(h8 *)(As + r * LD + c) = va[j];
-                *(h8 *)(Bs + r * LD + c) = vb[j];
-            }
-            __syncthreads();
-#pragma unroll
-            for (u32 kk = 0; kk < KT; kk += 32u) {
-                h8 fa[4], fb[4];
-#pragma unroll
-                for (u32 t = 0; t < 4u; t++) {
-                    fa[t] = *(const h8 *)(As + (wm + t * 16u + (lane & 15u)) * LD + kk + (lane >> 4) * 8u);
-                    fb[t] = *(const h8 *)(Bs + (wn + t * 16u + (lane & 15u)) * LD + kk + (lane >> 4) * 8u);
-                }
-                // (the columns of C are the rows of the instruction's result: a lane gets four consecutive ones)
-#pragma unroll
-                for (u32 i = 0; i < 4u; i++)
-#pragma unroll
-                    for (u32 j = 0; j < 4u; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        __syncthreads();
+        const u32 n = n0 + wn + (lane & 7u) * 8u;
+#pragma unroll 1
+        for (u32 q = 0; q < 8u; q++) {
+            const u32 r = q * 8u + (lane >> 3), m = m0 + wm + half * 64u + r, c = (lane & 7u) * 2u;
+            if (m >= g.M || n >= g.N) continue;
+            float v[8];
+            *(f4 *)v = *(const f4 *)(mine + r * 64u + (c ^ (r & 15u)) * 4u);
+            *(f4 *)(v + 4) = *(const f4 *)(mine + r * 64u + ((c + 1u) ^ (r & 15u)) * 4u);
+            if (g.partial) {
+                float *to = g.partial + ((u64)split * g.M + m) * g.n8 + n;
+                *(f4 *)to = *(const f4 *)v;
+                *(f4 *)(to + 4) = *(const f4 *)(v + 4);
+            } else {
+                scaled8<TY>(g, m, n, v, inv_w);
             }
         }
+    }
+}
+
+// The sums of the splits, in their order.
+template <u32 TY>
+__global__ __launch_bounds__(256) void k_join(Gemm g)
+{
     float s, inv_w = 1.0f;
     if (!g.inv_b) weight_scale(g.wpart, s, inv_w);
+    const u32 parts = g.n8 / 8u;
+    const u64 all = (u64)g.M * parts;
+    for (u64 i = blockIdx.x * 256ull + threadIdx.x; i < all; i += (u64)gridDim.x * 256u) {
+        const u32 m = (u32)(i / parts), n = (u32)(i - (u64)m * parts) * 8u;
+        float v[8] = {};
+        for (u32 q = 0; q < g.splits; q++) {
+            const GLOBAL_AS f4 *p = (const GLOBAL_AS f4 *)(gptr(g.partial) + ((u64)q * g.M + m) * g.n8 + n);
+            const f4 x = p[0], y = p[1];
 #pragma unroll
-    for (u32 i = 0; i < 4u; i++) {
-        const u32 m = m0 + wm + i * 16u + (lane & 15u);
-        if (m >= g.M) continue;
-        const float inv_a = gptr(g.inv_a)[m];
-#pragma unroll
-        for (u32 j = 0; j < 4u; j++) {
-            const u32 n = n0 + wn + j * 16u + (lane >> 4) * 4u;
-            if (n >= g.N) continue;
-            f4 v = acc[i][j];
-#pragma unroll
-            for (u32 t = 0; t < 4u; t++) v[t] = v[t] * inv_a * (g.inv_b ? (n + t < g.N ? gptr(g.inv_b)[n + t] : 0.0f) : inv_w);
-            epilogue4<TY>(g.end, m, n, v);
+            for (int t = 0; t < 4; t++) {
+                v[t] += x[t];
+                v[t + 4] += y[t];
+            }
         }
+        scaled8<TY>(g, m, n, v, inv_w);
     }
 }
 
@@ -406,7 +487,45 @@ void weight_planes(const WDesc &w, bool along, const Planes &p, char *ws, u64 pa
         along ? weight_planes_of<1, false>(w, p, ws, part, s) : weight_planes_of<1, true>(w, p, ws, part, s);
 }
 
-void product(Gemm g, const Planes &a, const Planes &b, char *ws, hipStream_t s)
+// How a product is cut: tiles of 256 x 256 or 128 x 128, and the reduction among several workgroups where there are few tiles.
+struct Cut {
+    bool large;
+    u32 m_tiles, n_tiles, splits, steps;
+    u64 partial; // bytes
+};
+constexpr u32 CUS = 256;
+Cut cut_of(u64 M, u64 N, u64 ld)
+{
+    Cut c;
+    const u64 big = up(M, 256) / 256 * (up(N, 256) / 256);
+    c.large = big >= CUS;
+    const u32 side = c.large ? 256u : 128u;
+    c.m_tiles = (u32)((M + side - 1) / side);
+    c.n_tiles = (u32)((N + side - 1) / side);
+    const u64 tiles = (u64)c.m_tiles * c.n_tiles, steps = ld / KT;
+    c.splits = 1;
+    while (!c.large && c.splits < 8u && tiles * c.splits < CUS && steps / (2u * c.splits) >= 4u) c.splits *= 2u;
+    c.steps = (u32)((steps + c.splits - 1) / c.splits);
+    c.splits = (u32)((steps + c.steps - 1) / c.steps); // (none without a step)
+    c.partial = c.splits > 1 ? up(N, 8) * M * c.splits * 4u : 0;
+    return c;
+}
+
+template <u32 TY>
+void product_of(const Gemm &g, const Cut &c, hipStream_t s)
+{
+    const u32 grid = c.m_tiles * c.n_tiles * c.splits;
+    if (c.large)
+        PROF("k_product", s, k_product<TY, 256, 256, 128, 64><<<grid, 512, 0, s>>>(g));
+    else
+        PROF("k_product", s, k_product<TY, 128, 128, 64, 64><<<grid, 256, 0, s>>>(g));
+    if (c.splits > 1) {
+        const u64 all = (u64)g.M * (g.n8 / 8u), blocks = (all + 255) / 256;
+        PROF("k_join", s, k_join<TY><<<(u32)(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(g));
+    }
+}
+
+void product(Gemm g, const Planes &a, const Planes &b, u64 partial, char *ws, hipStream_t s)
 {
     g.a = (const _Float16 *)(ws + a.off);
     g.b = (const _Float16 *)(ws + b.off);
@@ -419,12 +538,17 @@ void product(Gemm g, const Planes &a, const Planes &b, char *ws, hipStream_t s)
     if (a.count > 1) g.pa |= 1u << g.pairs++;
     if (b.count > 1) g.pb |= 1u << g.pairs++;
     g.pairs++;
-    g.n_tiles = (g.N + RT - 1) / RT;
-    const u32 grid = g.n_tiles * ((g.M + RT - 1) / RT);
+    const Cut c = cut_of(g.M, g.N, a.ld);
+    g.m_tiles = c.m_tiles;
+    g.n_tiles = c.n_tiles;
+    g.splits = c.splits;
+    g.steps = c.steps;
+    g.n8 = (u32)up(g.N, 8);
+    g.partial = c.splits > 1 ? (float *)(ws + partial) : nullptr;
     switch (g.type) {
-    case TY_F32: PROF("k_product", s, k_product<TY_F32><<<grid, 256, 0, s>>>(g)); break;
-    case TY_BF16: PROF("k_product", s, k_product<TY_BF16><<<grid, 256, 0, s>>>(g)); break;
-    default: PROF("k_product", s, k_product<TY_F16><<<grid, 256, 0, s>>>(g)); break;
+    case TY_F32: product_of<TY_F32>(g, c, s); break;
+    case TY_BF16: product_of<TY_BF16>(g, c, s); break;
+    default: product_of<TY_F16>(g, c, s); break;
     }
 }
 
@@ -434,18 +558,19 @@ u32 planes_w(u32 type) { return type == TY_BF16 ? 1u : 2u; }
 
 struct LinearRoom {
     Planes x, w;
-    u64 part, bytes;
+    u64 part, partial, bytes;
     LinearRoom(u64 rows, u32 n_in, u32 n_out, u32 type)
     {
         Room r;
         x = planes_for(r, rows, n_in, planes_x(type));
         w = planes_for(r, n_out, n_in, planes_w(type));
         part = r.take(WMAX_PARTS * 4u);
+        partial = r.take(cut_of(rows, n_out, x.ld).partial);
         bytes = r.at;
     }
 };
 struct GradRoom {
-    u64 d = 0, part = 0, bytes = 0;
+    u64 d = 0, part = 0, partial = 0, bytes = 0;
     Planes dr, w, dc, xc;
     bool own_d;
     GradRoom(u64 rows, u32 n_in, u32 n_out, u32 type, u32 act, bool dx, bool dw)
@@ -463,6 +588,10 @@ struct GradRoom {
             dc = planes_for(r, n_out, rows, planes_x(dt));
             xc = planes_for(r, n_in, rows, planes_x(type));
         }
+        // (the two products take turns)
+        u64 most = dx ? cut_of(rows, n_in, dr.ld).partial : 0;
+        if (dw) most = std::max(most, std::max(cut_of(n_out, n_in, dc.ld).partial, cut_of(n_in, n_out, dc.ld).partial));
+        partial = r.take(most);
         bytes = r.at;
     }
 };
@@ -492,7 +621,7 @@ hipError_t launch_linear(const LinearCall &c, hipStream_t s)
     g.wpart = (const u32 *)(c.ws + r.part);
     g.end = {c.bias, c.residual, c.y, c.pre, c.n_out, c.act};
     g.type = c.type;
-    product(g, r.x, r.w, c.ws, s);
+    product(g, r.x, r.w, r.partial, c.ws, s);
     return hipGetLastError();
 }
 
@@ -527,7 +656,7 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
         g.wpart = (const u32 *)(c.ws + r.part);
         g.end = {nullptr, {}, c.dx, {}, c.n_in, ACT_NONE};
         g.type = c.type;
-        product(g, r.dr, r.w, c.ws, s);
+        product(g, r.dr, r.w, r.partial, c.ws, s);
     }
     if (c.dw) {
         const PlaneSrc x = {c.x.p, nullptr, c.x.stride, 0, (u32)c.rows, c.n_in, ACT_NONE};
@@ -542,7 +671,7 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
         g.inv_b = (const float *)(c.ws + b.inv);
         g.end = {nullptr, {}, {c.dw, g.N}, {}, g.N, ACT_NONE};
         g.type = TY_F32;
-        product(g, a, b, c.ws, s);
+        product(g, a, b, r.partial, c.ws, s);
     }
     return hipGetLastError();
 }

@@ -96,21 +96,30 @@ struct Finish {
     u32 N, act;
 };
 
-// Results (m, n) .. (m, n + 3), the columns past N left out.
+// Results (m, n) .. (m, n + 7), n < N, the columns past N left out: bias, activation, residual, one rounding.
 template <u32 TY>
-__device__ __forceinline__ void epilogue4(const Finish &g, u32 m, u32 n, const f4 &v)
+__device__ __forceinline__ void finish8(const Finish &g, u32 m, u32 n, float (&v)[8])
 {
     typedef typename Elem<TY>::type T;
+    const u32 there = min(g.N - n, 8u);
+    if (g.bias) {
+        float b[8];
+        load8<TY_F32>(gptr(g.bias) + n, there, b);
 #pragma unroll
-    for (u32 i = 0; i < 4u; i++) {
-        if (n + i >= g.N) break;
-        float a = v[i];
-        if (g.bias) a += gptr(g.bias)[n + i];
-        if (g.pre.p) ((GLOBAL_AS T *)g.pre.p)[(u64)m * g.pre.stride + n + i] = Elem<TY>::put(a);
-        float y = act_of(a, g.act);
-        if (g.residual.p) y += Elem<TY>::get(((const GLOBAL_AS T *)g.residual.p)[(u64)m * g.residual.stride + n + i]);
-        ((GLOBAL_AS T *)g.out.p)[(u64)m * g.out.stride + n + i] = Elem<TY>::put(y);
+        for (int i = 0; i < 8; i++) v[i] += b[i];
     }
+    if (g.pre.p) store8<TY>((GLOBAL_AS T *)g.pre.p + (u64)m * g.pre.stride + n, there, v);
+    if (g.act != ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = act_of(v[i], g.act);
+    }
+    if (g.residual.p) {
+        float r[8];
+        load8<TY>((const GLOBAL_AS T *)g.residual.p + (u64)m * g.residual.stride + n, there, r);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] += r[i];
+    }
+    store8<TY>((GLOBAL_AS T *)g.out.p + (u64)m * g.out.stride + n, there, v);
 }
 
 } // namespace inshr

@@ -106,6 +106,17 @@ def test_shapes(ctx, shape, in_out, dtype):
     check_grad(ctx, layer, W, x, rows_of(rng, rows, n_out, dtype), rows_of(rng, rows, n_out, dtype))
 
 
+@pytest.mark.parametrize("rows,n_in,n_out,in_out", [(2100, 130, 8200, False), (2049, 200, 8000, True), (70, 4200, 4100, False),
+                                                    (66, 4097, 4500, True), (260, 9000, 70, False), (4100, 66, 130, True)])
+def test_large_shapes(ctx, rows, n_in, n_out, in_out):
+    """Many tiles, or few with a long reduction."""
+    rng = np.random.default_rng(rows)
+    for dtype in (BF16, F32):
+        layer, W, x, r = case(rng, rows, n_in, n_out, 16, dtype, "silu", in_out, residual=True, protected=5000)
+        check_linear(ctx, layer, W, x, r)
+        check_grad(ctx, layer, W, x, rows_of(rng, rows, n_out, dtype), rows_of(rng, rows, n_out, dtype))
+
+
 @pytest.mark.parametrize("bins", [2, 3, 4, 6, 8, 12, 16, 32, 64, 128, 256])
 @pytest.mark.parametrize("rows", [1, 9, 70])
 def test_numbers_of_bins(ctx, bins, rows):
