@@ -17,7 +17,7 @@
 //
 // Protected values are 0 in the table and are added at the end, from the list, in fixed point: whole numbers add up to
 // the same sum in any order.
-#include "inshr_product.h"
+#include "inshr_table.h"
 
 namespace inshr {
 
@@ -31,88 +31,8 @@ union Frag { // eight numbers of 16 bits
 };
 
 // ------------------------------------------------------------------------------------------
-// the table
+// operands
 // ------------------------------------------------------------------------------------------
-// Copies of an entry, one per bank (or two) that the lanes of a read meet in; at most 16 KB in all.
-template <u32 TY, int W> struct Table {
-    static constexpr u32 WORDS = TY == TY_F32 ? 2u : 1u; // 32-bit words of an entry
-    static constexpr u32 COPIES = (W <= 7 ? 32u : W == 8 ? 16u : 8u) / WORDS;
-    static constexpr u32 BYTES = (1u << W) * COPIES * WORDS * 4u;
-};
-__device__ __forceinline__ u32 bf16_cut(float x) { return __float_as_uint(x) & 0xffff0000u; } // towards zero: what is left over is exact
-template <u32 TY>
-__device__ __forceinline__ void entry_of(float v, float s, u32 (&e)[2])
-{
-    if (TY == TY_BF16) {
-        const u32 hi = Elem<TY_BF16>::put(v);
-        const float rest = v - __uint_as_float(hi << 16);
-        e[0] = hi | (u32)Elem<TY_BF16>::put(rest) << 16;
-    } else if (TY == TY_F16) {
-        union { _Float16 h; u16 u; } a, b;
-        a.h = (_Float16)(v * s);
-        b.h = (_Float16)(v * s - (float)a.h);
-        e[0] = a.u | (u32)b.u << 16;
-    } else {
-        const u32 h = bf16_cut(v);
-        const float r1 = v - __uint_as_float(h);
-        const u32 m = bf16_cut(r1);
-        e[0] = h >> 16 | m;
-        e[1] = __float_as_uint(r1 - __uint_as_float(m)) >> 16;
-    }
-}
-// Fills the table; returns what results are to be multiplied by.  A barrier has to follow.
-template <u32 TY, int W>
-__device__ __forceinline__ float fill_table(const WDesc &w, u32 *table)
-{
-    typedef Table<TY, W> T;
-    float s = 1.0f, inv = 1.0f;
-    if (TY == TY_F16) {
-        u32 m = 0u;
-        for (u32 i = threadIdx.x & 63u; i < w.K; i += 64u) m = max(m, finite_mag(gptr(w.codebook)[i]));
-        scale_of(wave_max_u(m), s, inv);
-    }
-    constexpr u32 C = T::COPIES;
-    for (u32 i = threadIdx.x; i < (1u << W) * C; i += blockDim.x) {
-        u32 e[2];
-        entry_of<TY>(symbol_value(w, i / C), s, e);
-        table[i * T::WORDS] = e[0];
-        if (T::WORDS > 1) table[i * T::WORDS + 1] = e[1];
-    }
-    return inv;
-}
-// where this lane's copy of entry 0 is (bytes)
-template <u32 TY, int W>
-__device__ __forceinline__ u32 lane_copy()
-{
-    return (threadIdx.x & (Table<TY, W>::COPIES - 1u)) * Table<TY, W>::WORDS * 4u;
-}
-// The entry of symbol j of a run whose first bit is bit 0 of d[0].
-template <u32 TY, int W>
-__device__ __forceinline__ void look_up(const char *table, u32 mine, const u32 *d, int j, u32 (&e)[2])
-{
-    typedef Table<TY, W> T;
-    constexpr int SH = __builtin_ctz(T::COPIES * T::WORDS * 4u); // an entry's copies: 2^SH bytes
-    constexpr u32 MASK = ((1u << W) - 1u) << SH;
-    const int bit = j * W, at = bit >> 5, off = bit & 31;
-    u32 a;
-    if (off + W > 32) // in two words
-        a = __builtin_amdgcn_alignbit(d[at + 1], d[at], (u32)off) << SH;
-    else if (off >= SH)
-        a = d[at] >> (off - SH);
-    else
-        a = d[at] << (SH - off);
-    const char *p = table + ((a & MASK) | mine);
-    if (T::WORDS > 1) {
-        const uint2 v = *(const uint2 *)p;
-        e[0] = v.x;
-        e[1] = v.y;
-    } else {
-        e[0] = *(const u32 *)p;
-    }
-}
-__device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-__device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-
 // The parts of eight values, by falling size, from their entries.
 template <u32 TY> struct Parts {
     static constexpr int N = TY == TY_F32 ? 3 : 2;
@@ -176,32 +96,6 @@ __device__ __forceinline__ f4 multiply(const Parts<TY> &w, const Xs<TY> &x, f4 c
 }
 
 // ------------------------------------------------------------------------------------------
-// the stream
-// ------------------------------------------------------------------------------------------
-typedef u32 u4_any __attribute__((ext_vector_type(4), aligned(4)));
-// N consecutive words, those from word `end` on as 0.
-template <int N>
-__device__ __forceinline__ void load_words(const u32 *packed, u64 at, u64 end, u32 *d)
-{
-    const GLOBAL_AS u32 *p = gptr(packed) + at;
-    if (at + N <= end) {
-#pragma unroll
-        for (int i = 0; i + 4 <= N; i += 4) {
-            const u4_any v = *(const GLOBAL_AS u4_any *)(p + i);
-            d[i] = v.x;
-            d[i + 1] = v.y;
-            d[i + 2] = v.z;
-            d[i + 3] = v.w;
-        }
-#pragma unroll
-        for (int i = N & ~3; i < N; i++) d[i] = p[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i++) d[i] = at + i < end ? p[i] : 0u;
-    }
-}
-
-// ------------------------------------------------------------------------------------------
 // protected values
 // ------------------------------------------------------------------------------------------
 // The first entry of the list that is not below `index`, by the lanes of half a wave: 32 places of what is left are
@@ -229,6 +123,14 @@ struct Few {
     u32 sums_at;     // byte offsets into LDS: the joined sums, ...
     u32 listed_at;   // ... the protected values' part of them
 };
+
+// The scale of the centres alone, by every wave.
+__device__ __forceinline__ void centre_scale(const WDesc &w, float &s, float &inv)
+{
+    u32 m = 0u;
+    for (u32 i = threadIdx.x & 63u; i < w.K; i += 64u) m = max(m, finite_mag(gptr(w.codebook)[i]));
+    scale_of(wave_max_u(m), s, inv);
+}
 
 // The joined sums of a workgroup, cols of them per row, lie at `sums`; adds the protected values' part and stores the
 // results.  lo .. hi: the entries of the list that may belong to the workgroup.
@@ -306,7 +208,9 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
     f4 *part = (f4 *)(lds + Table<TY, W>::BYTES);
     const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, waves = (blockDim.x >> 6) - 1u;
     const u32 n0 = blockIdx.x / f.row_blocks * 16u, m0 = blockIdx.x % f.row_blocks * (16u * MT);
-    const float inv = fill_table<TY, W>(f.w, table);
+    float s = 1.0f, inv = 1.0f;
+    if (TY == TY_F16) centre_scale(f.w, s, inv);
+    fill_table<TY, W>(f.w, table, s);
     __syncthreads();
     f4 acc[MT] = {};
     if (wave == waves) {
@@ -384,7 +288,9 @@ __global__ __launch_bounds__(1024) void k_few_cols(Few f)
     f4 *part = (f4 *)(lds + Table<TY, W>::BYTES);
     const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, waves = blockDim.x >> 6;
     const u32 n0 = blockIdx.x / f.row_blocks * (16u * R), m0 = blockIdx.x % f.row_blocks * (16u * MT);
-    const float inv = fill_table<TY, W>(f.w, table);
+    float s = 1.0f, inv = 1.0f;
+    if (TY == TY_F16) centre_scale(f.w, s, inv);
+    fill_table<TY, W>(f.w, table, s);
     __syncthreads();
     const u32 i = lane & 15u, g = lane >> 4, K = f.n_in;
     const u32 mine = lane_copy<TY, W>();
@@ -478,29 +384,15 @@ void start(Few &f, hipStream_t s)
     else
         start_cols_of<TY, W, MT, TY == TY_F32 ? 2 : 4>(f, s);
 }
-template <u32 TY, int MT>
-void start_w(Few &f, hipStream_t s)
-{
-    switch (f.w.w) {
-    case 2: start<TY, 2, MT>(f, s); break;
-    case 3: start<TY, 3, MT>(f, s); break;
-    case 4: start<TY, 4, MT>(f, s); break;
-    case 5: start<TY, 5, MT>(f, s); break;
-    case 6: start<TY, 6, MT>(f, s); break;
-    case 7: start<TY, 7, MT>(f, s); break;
-    case 8: start<TY, 8, MT>(f, s); break;
-    default: start<TY, 9, MT>(f, s); break;
-    }
-}
 template <u32 TY>
 void start_mt(Few &f, hipStream_t s)
 {
     if (f.rows <= 16u) {
         f.row_blocks = 1;
-        start_w<TY, 1>(f, s);
+        with_width(f.w.w, [&](auto w) { start<TY, decltype(w)::value, 1>(f, s); });
     } else {
         f.row_blocks = (f.rows + 31u) / 32u;
-        start_w<TY, 2>(f, s);
+        with_width(f.w.w, [&](auto w) { start<TY, decltype(w)::value, 2>(f, s); });
     }
 }
 

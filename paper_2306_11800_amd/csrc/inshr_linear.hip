@@ -9,7 +9,7 @@
 //   2 passes h h + h l          for fp16 results: fp16 activations are exact in h, the weight keeps 22 bits
 //   3 passes h h + h l + l h    for fp32 results: what is left out, l l, is 2^-22 of the product
 // (three planes of bfloat16 would need six passes for fp32, and two for bfloat16 results).
-#include "inshr_product.h"
+#include "inshr_table.h"
 
 #include <algorithm>
 
@@ -24,209 +24,345 @@ inline u64 up(u64 v, u64 to) { return (v + to - 1) / to * to; }
 struct PlaneSrc { // a matrix of elements; act != ACT_NONE: multiplied by the slope at the values of `pre`
     const void *p, *pre;
     u64 stride, pre_stride;
-    u32 rows, cols, act;
+    u32 rows, cols, act, pad;
 };
 
-// One workgroup per row.
+// The largest magnitudes of the centres and of parts of the protected list, to be joined by whoever needs the scale.
+constexpr u32 WMAX_PARTS = 64;
+__device__ __forceinline__ void weight_max_part(const WDesc &w, u32 which, u32 *part)
+{
+    u32 m = 0u;
+    if (which == 0 && threadIdx.x < w.K) m = finite_mag(gptr(w.codebook)[threadIdx.x]);
+    for (u64 j = which * 256ull + threadIdx.x; j < w.n_outlier; j += 256ull * WMAX_PARTS) m = max(m, finite_mag(protected_value(w, j)));
+    __shared__ u32 red[4];
+    m = wave_max_u(m);
+    if ((threadIdx.x & 63u) == 0u) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) part[which] = max(max(red[0], red[1]), max(red[2], red[3]));
+}
+__device__ __forceinline__ void weight_scale(const u32 *part, float &s, float &inv) // by every wave
+{
+    scale_of(wave_max_u(gptr(part)[threadIdx.x & 63u]), s, inv);
+}
+
+// Eight scaled values as one or two planes.
+template <int P>
+__device__ __forceinline__ void put_planes(const float (&v)[8], float s, _Float16 *at, u64 plane)
+{
+    h8 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float x = v[i] * s;
+        hi[i] = (_Float16)x;
+        lo[i] = (_Float16)(x - (float)hi[i]);
+    }
+    *(h8 *)at = hi;
+    if (P > 1) *(h8 *)(at + plane) = lo;
+}
+
+// One workgroup per row, read twice; the first WMAX_PARTS workgroups look through the weight's values instead.
 template <u32 TY, int P>
-__global__ __launch_bounds__(256) void k_row_planes(PlaneSrc src, _Float16 *__restrict__ dst, u64 plane, u32 Cp, float *__restrict__ inv_out)
+__global__ __launch_bounds__(256) void k_row_planes(PlaneSrc src, _Float16 *__restrict__ dst, u64 plane, u32 Cp, float *__restrict__ inv_out,
+                                                    WDesc w, u32 *__restrict__ part)
 {
     typedef typename Elem<TY>::type T;
-    const u64 r = blockIdx.x;
+    if (blockIdx.x < WMAX_PARTS) {
+        weight_max_part(w, blockIdx.x, part);
+        return;
+    }
+    const u64 r = blockIdx.x - WMAX_PARTS;
     const GLOBAL_AS T *p = (const GLOBAL_AS T *)src.p + r * src.stride;
     __shared__ u32 red[4];
     u32 m = 0u;
     for (u32 c = threadIdx.x * 8u; c < src.cols; c += 2048u) {
-        float v[8];
-        load8<TY>(p + c, src.cols - c, v);
+        const Raw8<TY> x = load_raw8<TY>(p + c, src.cols - c);
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const u32 f = finite_mag(v[i]);
-            m = m > f ? m : f;
-        }
+        for (int i = 0; i < 8; i++) m = max(m, finite_mag(x[i]));
     }
     m = wave_max_u(m);
     if ((threadIdx.x & 63u) == 0u) red[threadIdx.x >> 6] = m;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; i++) m = m > red[i] ? m : red[i];
     float s, inv;
-    scale_of(m, s, inv);
+    scale_of(max(max(red[0], red[1]), max(red[2], red[3])), s, inv);
     if (threadIdx.x == 0) inv_out[r] = inv;
     for (u32 c = threadIdx.x * 8u; c < Cp; c += 2048u) {
         float v[8];
         load8<TY>(p + c, c < src.cols ? src.cols - c : 0u, v);
-        h8 hi, lo;
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const float x = v[i] * s;
-            hi[i] = (_Float16)x;
-            lo[i] = (_Float16)(x - (float)hi[i]);
-        }
-        *(h8 *)(dst + r * Cp + c) = hi;
-        if (P > 1) *(h8 *)(dst + plane + r * Cp + c) = lo;
+        put_planes<P>(v, s, dst + r * Cp + c, plane);
     }
 }
 
 // ------------------------------------------------------------------------------------------
-// columns: largest magnitudes, sums, and the slope applied
+// the gradient below the activation, and the activations turned round
 // ------------------------------------------------------------------------------------------
-// A workgroup takes 64 columns and all rows: the sums are in a fixed order.
+// Both are cut into tiles of 64 x 64.  k_tile_stats takes each tile's largest magnitudes per row and per column and its
+// sums per column; k_scales joins them, in a fixed order; k_tile_planes works the values out again (they come from the
+// caches, and two planes of them would be as much to write and read) and stores the planes, the turned ones through LDS.
+struct TileJob {
+    PlaneSrc src;
+    u32 col_tiles, row_tiles;
+    u32 *row_max, *col_max;  // [col_tiles][rows], [row_tiles][cols]; NULL: not wanted
+    float *col_sum;          // [row_tiles][cols]
+    float *inv_row, *inv_col, *sum; // joined
+    _Float16 *by_row, *by_col;      // planes [rows][ld_row], [cols][ld_col]
+    u64 plane_row, plane_col, ld_row, ld_col;
+};
+struct TileJobs {
+    TileJob job[2];
+    u32 tiles0, tiles; // of the first, of both
+};
+
+// Rows i / 8 and i / 8 + 32 of the tile, eight columns from i % 8 * 8 on, for thread i.
 template <u32 TY>
-__global__ __launch_bounds__(256) void k_col_stats(PlaneSrc src, float *__restrict__ d_out, float *__restrict__ inv_out,
-                                                   float *__restrict__ sum_out)
+__device__ __forceinline__ void tile_values(const PlaneSrc &src, u64 r0, u32 c0, float (&v)[2][8])
 {
     typedef typename Elem<TY>::type T;
-    const u32 c = blockIdx.x * 64u + (threadIdx.x & 63u), part = threadIdx.x >> 6;
-    __shared__ float sums[4][64];
-    __shared__ u32 mags[4][64];
-    float sum = 0.0f;
-    u32 m = 0u;
-    if (c < src.cols)
-        for (u64 r = part; r < src.rows; r += 4u) {
-            float v = Elem<TY>::get(((const GLOBAL_AS T *)src.p)[r * src.stride + c]);
-            if (src.act != ACT_NONE) v *= act_grad(Elem<TY>::get(((const GLOBAL_AS T *)src.pre)[r * src.pre_stride + c]), src.act);
-            if (d_out) d_out[r * src.cols + c] = v;
-            sum += v;
-            const u32 f = finite_mag(v);
-            m = m > f ? m : f;
+    const u32 c = c0 + (threadIdx.x & 7u) * 8u;
+#pragma unroll
+    for (u32 h = 0; h < 2u; h++) {
+        const u64 r = r0 + (threadIdx.x >> 3) + 32u * h;
+        const u32 left = r < src.rows && c < src.cols ? src.cols - c : 0u;
+        load8<TY>((const GLOBAL_AS T *)src.p + r * src.stride + c, left, v[h]);
+        if (src.act != ACT_NONE) {
+            float a[8];
+            load8<TY>((const GLOBAL_AS T *)src.pre + r * src.pre_stride + c, left, a);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[h][i] = left ? v[h][i] * act_grad(a[i], src.act) : 0.0f;
         }
-    sums[part][threadIdx.x & 63u] = sum;
-    mags[part][threadIdx.x & 63u] = m;
-    __syncthreads();
-    if (part == 0u && c < src.cols) {
-        const u32 l = threadIdx.x;
-        if (sum_out) sum_out[c] = (sums[0][l] + sums[1][l]) + (sums[2][l] + sums[3][l]);
-        u32 all = 0u;
-        for (int i = 0; i < 4; i++) all = all > mags[i][l] ? all : mags[i][l];
-        float s, inv;
-        scale_of(all, s, inv);
-        if (inv_out) inv_out[c] = inv;
     }
 }
 
-// The planes of the transposed matrix, [cols][Rp]: tiles of 64 x 64 through LDS.
-template <u32 TY, int P>
-__global__ __launch_bounds__(256) void k_col_planes(PlaneSrc src, const float *__restrict__ inv, _Float16 *__restrict__ dst, u64 plane, u64 Rp)
+template <u32 TY>
+__global__ __launch_bounds__(256) void k_tile_stats(TileJobs jobs, WDesc w, u32 *__restrict__ part)
 {
-    typedef typename Elem<TY>::type T;
-    __shared__ float tile[64][65];
-    const u32 row_tiles = (src.rows + 63u) / 64u;
-    const u64 r0 = blockIdx.x % row_tiles * 64ull;
-    const u32 c0 = blockIdx.x / row_tiles * 64u;
-    for (u32 i = threadIdx.x; i < 4096u; i += 256u) {
-        const u64 r = r0 + (i >> 6);
-        const u32 c = c0 + (i & 63u);
-        tile[i >> 6][i & 63u] = r < src.rows && c < src.cols ? Elem<TY>::get(((const GLOBAL_AS T *)src.p)[r * src.stride + c]) : 0.0f;
+    if (blockIdx.x >= jobs.tiles) {
+        weight_max_part(w, blockIdx.x - jobs.tiles, part);
+        return;
+    }
+    const bool second = blockIdx.x >= jobs.tiles0;
+    const TileJob &j = jobs.job[second];
+    const u32 tile = blockIdx.x - (second ? jobs.tiles0 : 0u), rt = tile / j.col_tiles, ct = tile - rt * j.col_tiles;
+    const u64 r0 = rt * 64ull;
+    const u32 c0 = ct * 64u, i = threadIdx.x;
+    float v[2][8];
+    tile_values<TY>(j.src, r0, c0, v);
+    __shared__ u32 mags[4][64];
+    __shared__ float sums[4][64];
+    u32 cm[8];
+    float cs[8];
+#pragma unroll
+    for (int q = 0; q < 8; q++) {
+        cm[q] = max(finite_mag(v[0][q]), finite_mag(v[1][q]));
+        cs[q] = v[0][q] + v[1][q];
+    }
+    if (j.row_max) {
+#pragma unroll
+        for (u32 h = 0; h < 2u; h++) {
+            u32 m = 0u;
+#pragma unroll
+            for (int q = 0; q < 8; q++) m = max(m, finite_mag(v[h][q]));
+#pragma unroll
+            for (int d = 4; d; d >>= 1) m = max(m, __shfl_xor(m, d));
+            const u64 r = r0 + (i >> 3) + 32u * h;
+            if ((i & 7u) == 0u && r < j.src.rows) j.row_max[(u64)ct * j.src.rows + r] = m;
+        }
+    }
+    // lanes 8, 16 and 32 apart hold the same columns
+#pragma unroll
+    for (int d = 8; d < 64; d <<= 1)
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            cm[q] = max(cm[q], __shfl_xor(cm[q], d));
+            cs[q] += __shfl_xor(cs[q], d);
+        }
+    if ((i & 63u) < 8u) {
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            mags[i >> 6][(i & 7u) * 8u + q] = cm[q];
+            sums[i >> 6][(i & 7u) * 8u + q] = cs[q];
+        }
     }
     __syncthreads();
-    for (u32 i = threadIdx.x; i < 512u; i += 256u) {
-        const u32 c = i >> 3, r = (i & 7u) * 8u;
-        if (c0 + c >= src.cols) continue;
-        const float s = 1.0f / inv[c0 + c]; // (a power of two)
-        h8 hi, lo;
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float x = tile[r + j][c] * s;
-            hi[j] = (_Float16)x;
-            lo[j] = (_Float16)(x - (float)hi[j]);
+    if (i < 64u && c0 + i < j.src.cols) {
+        if (j.col_max) j.col_max[(u64)rt * j.src.cols + c0 + i] = max(max(mags[0][i], mags[1][i]), max(mags[2][i], mags[3][i]));
+        if (j.col_sum) j.col_sum[(u64)rt * j.src.cols + c0 + i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+    }
+}
+
+// A thread per row and per column.
+__global__ __launch_bounds__(256) void k_scales(TileJobs jobs)
+{
+    u64 i = blockIdx.x * 256ull + threadIdx.x;
+    for (int q = 0; q < 2; q++) {
+        const TileJob &j = jobs.job[q];
+        if (!j.src.p) return;
+        if (i < j.src.rows) {
+            if (!j.row_max) return;
+            u32 m = 0u;
+#pragma unroll 4
+            for (u32 t = 0; t < j.col_tiles; t++) m = max(m, gptr(j.row_max)[(u64)t * j.src.rows + i]);
+            float s;
+            scale_of(m, s, j.inv_row[i]);
+            return;
         }
-        _Float16 *at = dst + (u64)(c0 + c) * Rp + r0 + r;
-        *(h8 *)at = hi;
-        if (P > 1) *(h8 *)(at + plane) = lo;
+        i -= j.src.rows;
+        if (i < j.src.cols) {
+            u32 m = 0u;
+            float sum = 0.0f, s;
+#pragma unroll 4
+            for (u32 t = 0; t < j.row_tiles; t++) {
+                if (j.col_max) m = max(m, gptr(j.col_max)[(u64)t * j.src.cols + i]);
+                if (j.col_sum) sum += gptr(j.col_sum)[(u64)t * j.src.cols + i];
+            }
+            if (j.col_max) scale_of(m, s, j.inv_col[i]);
+            if (j.col_sum) j.sum[i] = sum;
+            return;
+        }
+        i -= j.src.cols;
+    }
+}
+
+// P1, P2: planes by row and by column (of both jobs)
+template <u32 TY, int PR, int PC0, int PC1>
+__global__ __launch_bounds__(256) void k_tile_planes(TileJobs jobs)
+{
+    const bool second = blockIdx.x >= jobs.tiles0;
+    const TileJob &j = jobs.job[second];
+    const u32 tile = blockIdx.x - (second ? jobs.tiles0 : 0u), rt = tile / j.col_tiles, ct = tile - rt * j.col_tiles;
+    const u64 r0 = rt * 64ull;
+    const u32 c0 = ct * 64u, i = threadIdx.x;
+    float v[2][8];
+    tile_values<TY>(j.src, r0, c0, v);
+    if (j.by_row) {
+#pragma unroll
+        for (u32 h = 0; h < 2u; h++) {
+            const u64 r = r0 + (i >> 3) + 32u * h;
+            if (r < j.src.rows) put_planes<PR>(v[h], 1.0f / gptr(j.inv_row)[r], j.by_row + r * j.ld_row + c0 + (i & 7u) * 8u, j.plane_row);
+        }
+    }
+    if (j.by_col) {
+        __shared__ float lds[64][65];
+#pragma unroll
+        for (u32 h = 0; h < 2u; h++)
+#pragma unroll
+            for (u32 q = 0; q < 8u; q++) lds[(i >> 3) + 32u * h][(i & 7u) * 8u + q] = v[h][q];
+        __syncthreads();
+#pragma unroll
+        for (u32 h = 0; h < 2u; h++) {
+            const u32 c = (i >> 3) + 32u * h, r = (i & 7u) * 8u;
+            if (c0 + c >= j.src.cols) continue;
+            float x[8];
+#pragma unroll
+            for (u32 q = 0; q < 8u; q++) x[q] = lds[r + q][c];
+            const float s = 1.0f / gptr(j.inv_col)[c0 + c]; // (a power of two)
+            _Float16 *at = j.by_col + (u64)(c0 + c) * j.ld_col + r0 + r;
+            if (second)
+                put_planes<PC1>(x, s, at, j.plane_col);
+            else
+                put_planes<PC0>(x, s, at, j.plane_col);
+        }
     }
 }
 
 // ------------------------------------------------------------------------------------------
 // the weight
 // ------------------------------------------------------------------------------------------
-constexpr u32 WMAX_PARTS = 64;
-
-// largest magnitudes of the centres and of parts of the protected list
-__global__ __launch_bounds__(256) void k_weight_max(WDesc w, u32 *__restrict__ part)
+// Eight entries of the table into the planes, the marked ones left out.
+template <int P>
+__device__ __forceinline__ void store_entries(const u32 (&e)[8][2], u32 skip, _Float16 *at, u64 plane)
 {
-    u32 m = 0u;
-    if (blockIdx.x == 0 && threadIdx.x < w.K) m = finite_mag(gptr(w.codebook)[threadIdx.x]);
-    for (u64 j = blockIdx.x * 256ull + threadIdx.x; j < w.n_outlier; j += 256ull * WMAX_PARTS) {
-        const u32 f = finite_mag(protected_value(w, j));
-        m = m > f ? m : f;
-    }
-    __shared__ u32 red[4];
-    m = wave_max_u(m);
-    if ((threadIdx.x & 63u) == 0u) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 4; i++) m = m > red[i] ? m : red[i];
-        part[blockIdx.x] = m;
-    }
-}
-// the whole of k_weight_max's parts, by every wave
-__device__ __forceinline__ void weight_scale(const u32 *part, float &s, float &inv)
-{
-    scale_of(wave_max_u(gptr(part)[threadIdx.x & 63u]), s, inv);
-}
-
-// Symbol i of the stream; words past its end are not read.
-__device__ __forceinline__ u32 symbol_at(const WDesc &w, u64 i)
-{
-    const u64 bit = i * w.w, at = bit >> 5;
-    const u32 lo = gptr(w.packed)[at], hi = at + 1 < w.n_words ? gptr(w.packed)[at + 1] : 0u;
-    return __builtin_amdgcn_alignbit(hi, lo, (u32)bit & 31u) & ((1u << w.w) - 1u);
-}
-
-// Planes [rows][Cp] (T == false) or, transposed, [cols][Rp]; padding of the reduction is zero.
-template <int P, bool T>
-__global__ __launch_bounds__(256) void k_weight_planes(WDesc w, const u32 *__restrict__ part, _Float16 *__restrict__ dst, u64 plane, u64 ld)
-{
-    __shared__ _Float16 hi[512], lo[512];
-    __shared__ u16 sym[64][66];
-    float s, inv;
-    weight_scale(part, s, inv);
-    for (u32 i = threadIdx.x; i < 512u; i += 256u) {
-        const float x = symbol_value(w, i) * s;
-        hi[i] = (_Float16)x;
-        lo[i] = (_Float16)(x - (float)hi[i]);
-    }
-    const u32 col_tiles = (w.cols + 63u) / 64u;
-    const u64 r0 = blockIdx.x / col_tiles * 64ull;
-    const u32 c0 = blockIdx.x % col_tiles * 64u;
-    for (u32 i = threadIdx.x; i < 4096u; i += 256u) {
-        const u64 r = r0 + (i >> 6);
-        const u32 c = c0 + (i & 63u);
-        sym[i >> 6][i & 63u] = r < w.rows && c < w.cols ? (u16)symbol_at(w, r * w.cols + c) : (u16)0;
-    }
-    __syncthreads();
-    for (u32 i = threadIdx.x; i < 512u; i += 256u) {
-        const u32 a = i >> 3, b = (i & 7u) * 8u; // a: row of the planes, b: along the reduction
-        const u64 row = (T ? c0 : r0) + a;
-        if (row >= (T ? w.cols : w.rows)) continue;
-        h8 vh, vl;
+    u4_16 hi, lo;
 #pragma unroll
-        for (u32 j = 0; j < 8u; j++) {
-            const u32 q = T ? sym[b + j][a] : sym[a][b + j];
-            vh[j] = hi[q];
-            vl[j] = lo[q];
+    for (int q = 0; q < 4; q++) {
+        hi[q] = low_halves(e[2 * q][0], e[2 * q + 1][0]);
+        lo[q] = high_halves(e[2 * q][0], e[2 * q + 1][0]);
+    }
+    if (skip == 0u) {
+        *(u4_16 *)at = hi;
+        if (P > 1) *(u4_16 *)(at + plane) = lo;
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            if (skip >> q & 1u) continue;
+            ((u16 *)at)[q] = (u16)(hi[q / 2] >> (16 * (q & 1)));
+            if (P > 1) ((u16 *)(at + plane))[q] = (u16)(lo[q / 2] >> (16 * (q & 1)));
         }
-        _Float16 *at = dst + row * ld + (T ? r0 : c0) + b;
-        *(h8 *)at = vh;
-        if (P > 1) *(h8 *)(at + plane) = vl;
     }
 }
+constexpr u32 ONE_MARK = 0xFC00FC00u; // (minus infinity twice: no entry has a high part that is infinite and one that is left over)
 
-// The protected values into the planes (indices outside the weight are left out).
-template <int P, bool T>
-__global__ __launch_bounds__(256) void k_weight_protected(WDesc w, const u32 *__restrict__ part, _Float16 *__restrict__ dst, u64 plane, u64 ld)
+// Planes [rows][Cp] (T == false) or, turned, [cols][Rp]; padding of the reduction is zero.  A thread decodes runs of eight
+// symbols; protected places are left to the workgroups behind the tiles, which take them from the list (indices outside the
+// weight are left out).
+template <int W, int P, bool T>
+__global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const u32 *__restrict__ part, _Float16 *__restrict__ dst, u64 plane, u64 ld)
 {
+    typedef Table<TY_F16, W> Tab;
+    constexpr int ND = (8 * W + 31) / 32;
+    __shared__ __attribute__((aligned(16))) u32 table[Tab::BYTES / 4];
     float s, inv;
     weight_scale(part, s, inv);
-    for (u64 j = blockIdx.x * 256ull + threadIdx.x; j < w.n_outlier; j += (u64)gridDim.x * 256u) {
-        const u32 i = gptr(w.out_idx)[j], r = i / w.cols, c = i - r * w.cols;
-        if (r >= w.rows) continue;
-        const float x = protected_value(w, j) * s;
-        const _Float16 hi = (_Float16)x;
-        _Float16 *at = dst + (T ? (u64)c * ld + r : (u64)r * ld + c);
-        at[0] = hi;
-        if (P > 1) at[plane] = (_Float16)(x - (float)hi);
+    if (blockIdx.x >= tiles) {
+        for (u64 j = (blockIdx.x - tiles) * 256ull + threadIdx.x; j < w.n_outlier; j += (u64)(gridDim.x - tiles) * 256u) {
+            const u32 i = gptr(w.out_idx)[j], r = i / w.cols, c = i - r * w.cols;
+            if (r >= w.rows) continue;
+            const float x = protected_value(w, j) * s;
+            const _Float16 hi = (_Float16)x;
+            _Float16 *at = dst + (T ? (u64)c * ld + r : (u64)r * ld + c);
+            at[0] = hi;
+            if (P > 1) at[plane] = (_Float16)(x - (float)hi);
+        }
+        return;
+    }
+    fill_table<TY_F16, W>(w, table, s);
+    __syncthreads();
+    const u32 mine = lane_copy<TY_F16, W>();
+    // a tile of 64 rows x 128 columns: four runs a thread
+    constexpr u32 TILE_C = T ? 64u : 128u;
+    const u32 col_tiles = (w.cols + TILE_C - 1u) / TILE_C;
+    const u64 r0 = blockIdx.x / col_tiles * 64ull;
+    const u32 c0 = blockIdx.x % col_tiles * TILE_C;
+    __shared__ u32 turned[T ? 64 : 1][65];
+#pragma unroll
+    for (u32 h = 0; h < TILE_C / 32u; h++) {
+        const u32 i = threadIdx.x + 256u * h, run = i % (TILE_C / 8u), c = c0 + run * 8u;
+        const u64 r = r0 + i / (TILE_C / 8u);
+        const u32 left = r < w.rows && c < w.cols ? w.cols - c : 0u;
+        u32 raw[ND + 1], d[ND + 1];
+        const u64 bit = (r * w.cols + c) * W;
+        load_words<ND + 1>(w.packed, bit >> 5, left ? w.n_words : 0, raw);
+#pragma unroll
+        for (int q = 0; q < ND; q++) d[q] = __builtin_amdgcn_alignbit(raw[q + 1], raw[q], (u32)bit & 31u);
+        d[ND] = 0u;
+        u32 e[8][2];
+        u32 at_one = 0u; // protected places
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            look_up<TY_F16, W>((const char *)table, mine, d, q, e[q]);
+            if ((u32)q >= left) e[q][0] = 0u;
+            if (!T) at_one |= (symbol_of<W>(d, q) == 1u && (u32)q < left ? 1u : 0u) << q;
+        }
+        if (T) {
+#pragma unroll
+            for (int q = 0; q < 8; q++) turned[i / (TILE_C / 8u)][run * 8u + q] = symbol_of<W>(d, q) == 1u && (u32)q < left ? ONE_MARK : e[q][0];
+        } else if (r < w.rows && c < (u32)ld) {
+            store_entries<P>(e, at_one, dst + r * ld + c, plane);
+        }
+    }
+    if (T) {
+        __syncthreads();
+#pragma unroll
+        for (u32 h = 0; h < 2u; h++) {
+            const u32 i = threadIdx.x + 256u * h, c = i >> 3, r = (i & 7u) * 8u;
+            if (c0 + c >= w.cols) continue;
+            u32 e[8][2], at_one = 0u;
+#pragma unroll
+            for (u32 q = 0; q < 8u; q++) {
+                e[q][0] = turned[r + q][c];
+                at_one |= (e[q][0] == ONE_MARK ? 1u : 0u) << q;
+            }
+            store_entries<P>(e, at_one, dst + (u64)(c0 + c) * ld + r0 + r, plane);
+        }
     }
 }
 
@@ -419,72 +555,47 @@ Planes planes_for(Room &r, u64 rows, u64 reduction, u32 count)
     return p;
 }
 
-template <int P>
-void row_planes(const PlaneSrc &src, u32 type, const Planes &p, char *ws, hipStream_t s)
+// x's planes and the parts of the weight's largest magnitude
+template <u32 TY>
+void row_planes_of(const PlaneSrc &src, const Planes &p, const WDesc &w, u64 part, char *ws, hipStream_t s)
 {
     _Float16 *dst = (_Float16 *)(ws + p.off);
     float *inv = (float *)(ws + p.inv);
-    switch (type) {
-    case TY_F32: PROF("k_row_planes", s, k_row_planes<TY_F32, P><<<src.rows, 256, 0, s>>>(src, dst, p.plane, (u32)p.ld, inv)); break;
-    case TY_BF16: PROF("k_row_planes", s, k_row_planes<TY_BF16, P><<<src.rows, 256, 0, s>>>(src, dst, p.plane, (u32)p.ld, inv)); break;
-    default: PROF("k_row_planes", s, k_row_planes<TY_F16, P><<<src.rows, 256, 0, s>>>(src, dst, p.plane, (u32)p.ld, inv)); break;
-    }
-}
-void row_planes(const PlaneSrc &src, u32 type, const Planes &p, char *ws, hipStream_t s)
-{
+    u32 *pm = (u32 *)(ws + part);
     if (p.count > 1)
-        row_planes<2>(src, type, p, ws, s);
+        PROF("k_row_planes", s, k_row_planes<TY, 2><<<src.rows + WMAX_PARTS, 256, 0, s>>>(src, dst, p.plane, (u32)p.ld, inv, w, pm));
     else
-        row_planes<1>(src, type, p, ws, s);
+        PROF("k_row_planes", s, k_row_planes<TY, 1><<<src.rows + WMAX_PARTS, 256, 0, s>>>(src, dst, p.plane, (u32)p.ld, inv, w, pm));
 }
-
-template <u32 TY>
-void col_planes_of(const PlaneSrc &src, const Planes &p, char *ws, hipStream_t s)
+void row_planes(const PlaneSrc &src, u32 type, const Planes &p, const WDesc &w, u64 part, char *ws, hipStream_t s)
 {
-    const u32 grid = (src.rows + 63u) / 64u * ((src.cols + 63u) / 64u);
-    _Float16 *dst = (_Float16 *)(ws + p.off);
-    const float *inv = (const float *)(ws + p.inv);
-    if (p.count > 1)
-        PROF("k_col_planes", s, k_col_planes<TY, 2><<<grid, 256, 0, s>>>(src, inv, dst, p.plane, p.ld));
-    else
-        PROF("k_col_planes", s, k_col_planes<TY, 1><<<grid, 256, 0, s>>>(src, inv, dst, p.plane, p.ld));
-}
-void col_planes(const PlaneSrc &src, u32 type, const Planes &p, char *ws, hipStream_t s)
-{
-    type == TY_F32 ? col_planes_of<TY_F32>(src, p, ws, s) : type == TY_BF16 ? col_planes_of<TY_BF16>(src, p, ws, s) : col_planes_of<TY_F16>(src, p, ws, s);
-}
-void col_stats(const PlaneSrc &src, u32 type, float *d, float *inv, float *sum, hipStream_t s)
-{
-    const u32 grid = (src.cols + 63u) / 64u;
     switch (type) {
-    case TY_F32: PROF("k_col_stats", s, k_col_stats<TY_F32><<<grid, 256, 0, s>>>(src, d, inv, sum)); break;
-    case TY_BF16: PROF("k_col_stats", s, k_col_stats<TY_BF16><<<grid, 256, 0, s>>>(src, d, inv, sum)); break;
-    default: PROF("k_col_stats", s, k_col_stats<TY_F16><<<grid, 256, 0, s>>>(src, d, inv, sum)); break;
+    case TY_F32: row_planes_of<TY_F32>(src, p, w, part, ws, s); break;
+    case TY_BF16: row_planes_of<TY_BF16>(src, p, w, part, ws, s); break;
+    default: row_planes_of<TY_F16>(src, p, w, part, ws, s); break;
     }
 }
 
 // along: the reduction runs along the stored rows
-template <int P, bool T>
-void weight_planes_of(const WDesc &w, const Planes &p, char *ws, u64 part, hipStream_t s)
+void weight_planes(const WDesc &w, bool along, const Planes &p, char *ws, u64 part, hipStream_t s)
 {
     const u32 *pm = (const u32 *)(ws + part);
     _Float16 *dst = (_Float16 *)(ws + p.off);
-    PROF("k_weight_max", s, k_weight_max<<<WMAX_PARTS, 256, 0, s>>>(w, (u32 *)(ws + part)));
-    // (the padding along the reduction belongs to the grid: it is written as zeros)
-    const u32 grid = (w.cols + 63u) / 64u * ((w.rows + 63u) / 64u);
-    PROF("k_weight_planes", s, k_weight_planes<P, T><<<grid, 256, 0, s>>>(w, pm, dst, p.plane, p.ld));
-    if (w.n_outlier) {
-        u64 blocks = (w.n_outlier + 255) / 256;
-        if (blocks > 2048) blocks = 2048;
-        PROF("k_weight_protected", s, k_weight_protected<P, T><<<(u32)blocks, 256, 0, s>>>(w, pm, dst, p.plane, p.ld));
-    }
-}
-void weight_planes(const WDesc &w, bool along, const Planes &p, char *ws, u64 part, hipStream_t s)
-{
-    if (p.count > 1)
-        along ? weight_planes_of<2, false>(w, p, ws, part, s) : weight_planes_of<2, true>(w, p, ws, part, s);
-    else
-        along ? weight_planes_of<1, false>(w, p, ws, part, s) : weight_planes_of<1, true>(w, p, ws, part, s);
+    // (the padding along the reduction belongs to the tiles: it is written as zeros)
+    const u32 tile_c = along ? 128u : 64u, tiles = (w.cols + tile_c - 1u) / tile_c * ((w.rows + 63u) / 64u);
+    const u32 grid = tiles + (u32)std::min<u64>((w.n_outlier + 255) / 256, 512);
+    with_width(w.w, [&](auto width) {
+        constexpr int W = decltype(width)::value;
+        auto start = [&](auto planes, auto turned) {
+            PROF("k_weight_planes", s, k_weight_planes<W, decltype(planes)::value, decltype(turned)::value><<<grid, 256, 0, s>>>(w, tiles, pm, dst, p.plane, p.ld));
+        };
+        typedef std::integral_constant<int, 1> One;
+        typedef std::integral_constant<int, 2> Two;
+        if (p.count > 1)
+            along ? start(Two(), std::false_type()) : start(Two(), std::true_type());
+        else
+            along ? start(One(), std::false_type()) : start(One(), std::true_type());
+    });
 }
 
 // How a product is cut: tiles of 256 x 256 or 128 x 128, and the reduction among several workgroups where there are few tiles.
@@ -570,23 +681,27 @@ struct LinearRoom {
     }
 };
 struct GradRoom {
-    u64 d = 0, part = 0, partial = 0, bytes = 0;
-    Planes dr, w, dc, xc;
-    bool own_d;
+    u64 part = 0, partial = 0, bytes = 0;
+    u64 row_max = 0, col_max = 0, col_sum = 0, x_max = 0;
+    Planes dr = {}, w = {}, dc = {}, xc = {};
     GradRoom(u64 rows, u32 n_in, u32 n_out, u32 type, u32 act, bool dx, bool dw)
     {
         Room r;
-        own_d = act != ACT_NONE; // the gradient below the activation, in fp32
-        if (own_d) d = r.take(rows * n_out * 4u);
-        const u32 dt = own_d ? TY_F32 : type;
+        const u64 row_tiles = up(rows, 64) / 64, col_tiles = up(n_out, 64) / 64;
+        // d is what it is in its type, or, below an activation, an fp32 number
+        const u32 dt = act != ACT_NONE ? TY_F32 : type;
+        col_sum = r.take(row_tiles * n_out * 4u);
         if (dx) {
             dr = planes_for(r, rows, n_out, type == TY_BF16 ? 1u : planes_x(dt));
             w = planes_for(r, n_in, n_out, planes_w(type));
             part = r.take(WMAX_PARTS * 4u);
+            row_max = r.take(col_tiles * rows * 4u);
         }
         if (dw) { // (fp32 results)
             dc = planes_for(r, n_out, rows, planes_x(dt));
             xc = planes_for(r, n_in, rows, planes_x(type));
+            col_max = r.take(row_tiles * n_out * 4u);
+            x_max = r.take(row_tiles * n_in * 4u);
         }
         // (the two products take turns)
         u64 most = dx ? cut_of(rows, n_in, dr.ld).partial : 0;
@@ -595,6 +710,18 @@ struct GradRoom {
         bytes = r.at;
     }
 };
+
+template <u32 TY>
+void tile_planes(const TileJobs &t, u32 dr, u32 dc, hipStream_t s)
+{
+    constexpr int PX = TY == TY_F32 ? 2 : 1;
+    if (dr > 1)
+        PROF("k_tile_planes", s, k_tile_planes<TY, 2, 2, PX><<<t.tiles, 256, 0, s>>>(t));
+    else if (dc > 1)
+        PROF("k_tile_planes", s, k_tile_planes<TY, 1, 2, PX><<<t.tiles, 256, 0, s>>>(t));
+    else
+        PROF("k_tile_planes", s, k_tile_planes<TY, 1, 1, PX><<<t.tiles, 256, 0, s>>>(t));
+}
 
 } // namespace
 
@@ -612,7 +739,7 @@ hipError_t launch_linear(const LinearCall &c, hipStream_t s)
     if (is_few(c.rows)) return launch_few(c, s);
     const LinearRoom r(c.rows, c.n_in, c.n_out, c.type);
     const PlaneSrc x = {c.x.p, nullptr, c.x.stride, 0, (u32)c.rows, c.n_in, ACT_NONE};
-    row_planes(x, c.type, r.x, c.ws, s);
+    row_planes(x, c.type, r.x, c.w, r.part, c.ws, s);
     weight_planes(c.w, !c.in_out, r.w, c.ws, r.part, s);
     Gemm g = {};
     g.M = (u32)c.rows;
@@ -638,16 +765,53 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
         return hipGetLastError();
     }
     const GradRoom r(c.rows, c.n_in, c.n_out, c.type, c.act, c.dx.p != nullptr, c.dw != nullptr);
-    PlaneSrc d = {c.dy.p, c.pre.p, c.dy.stride, c.pre.stride, (u32)c.rows, c.n_out, c.act};
-    u32 dt = c.type;
-    if (r.own_d || c.dw || c.db)
-        col_stats(d, c.type, r.own_d ? (float *)(c.ws + r.d) : nullptr, c.dw ? (float *)(c.ws + r.dc.inv) : nullptr, c.db, s);
-    if (r.own_d) {
-        d = {c.ws + r.d, nullptr, c.n_out, 0, (u32)c.rows, c.n_out, ACT_NONE};
-        dt = TY_F32;
+    const bool dx = c.dx.p != nullptr, dw = c.dw != nullptr;
+    TileJobs t = {};
+    TileJob &d = t.job[0], &x = t.job[1];
+    d.src = {c.dy.p, c.pre.p, c.dy.stride, c.pre.stride, (u32)c.rows, c.n_out, c.act, 0};
+    d.col_tiles = (c.n_out + 63u) / 64u;
+    d.row_tiles = ((u32)c.rows + 63u) / 64u;
+    d.sum = c.db;
+    if (c.db) d.col_sum = (float *)(c.ws + r.col_sum);
+    if (dx) {
+        d.row_max = (u32 *)(c.ws + r.row_max);
+        d.inv_row = (float *)(c.ws + r.dr.inv);
+        d.by_row = (_Float16 *)(c.ws + r.dr.off);
+        d.plane_row = r.dr.plane;
+        d.ld_row = r.dr.ld;
     }
-    if (c.dx.p) {
-        row_planes(d, dt, r.dr, c.ws, s);
+    t.tiles0 = t.tiles = d.col_tiles * d.row_tiles;
+    if (dw) {
+        d.col_max = (u32 *)(c.ws + r.col_max);
+        d.inv_col = (float *)(c.ws + r.dc.inv);
+        d.by_col = (_Float16 *)(c.ws + r.dc.off);
+        d.plane_col = r.dc.plane;
+        d.ld_col = r.dc.ld;
+        x.src = {c.x.p, nullptr, c.x.stride, 0, (u32)c.rows, c.n_in, ACT_NONE, 0};
+        x.col_tiles = (c.n_in + 63u) / 64u;
+        x.row_tiles = d.row_tiles;
+        x.col_max = (u32 *)(c.ws + r.x_max);
+        x.inv_col = (float *)(c.ws + r.xc.inv);
+        x.by_col = (_Float16 *)(c.ws + r.xc.off);
+        x.plane_col = r.xc.plane;
+        x.ld_col = r.xc.ld;
+        t.tiles += x.col_tiles * x.row_tiles;
+    }
+    u32 *part = dx ? (u32 *)(c.ws + r.part) : nullptr;
+    const u32 grid = t.tiles + (dx ? WMAX_PARTS : 0u);
+    const u64 lines = c.rows + c.n_out + (dw ? c.rows + c.n_in : 0u);
+    switch (c.type) {
+    case TY_F32: PROF("k_tile_stats", s, k_tile_stats<TY_F32><<<grid, 256, 0, s>>>(t, c.w, part)); break;
+    case TY_BF16: PROF("k_tile_stats", s, k_tile_stats<TY_BF16><<<grid, 256, 0, s>>>(t, c.w, part)); break;
+    default: PROF("k_tile_stats", s, k_tile_stats<TY_F16><<<grid, 256, 0, s>>>(t, c.w, part)); break;
+    }
+    PROF("k_scales", s, k_scales<<<(u32)((lines + 255) / 256), 256, 0, s>>>(t));
+    if (dx || dw) switch (c.type) {
+    case TY_F32: tile_planes<TY_F32>(t, r.dr.count, r.dc.count, s); break;
+    case TY_BF16: tile_planes<TY_BF16>(t, r.dr.count, r.dc.count, s); break;
+    default: tile_planes<TY_F16>(t, r.dr.count, r.dc.count, s); break;
+    }
+    if (dx) {
         weight_planes(c.w, c.in_out, r.w, c.ws, r.part, s);
         Gemm g = {};
         g.M = (u32)c.rows;
@@ -658,11 +822,7 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
         g.type = c.type;
         product(g, r.dr, r.w, r.partial, c.ws, s);
     }
-    if (c.dw) {
-        const PlaneSrc x = {c.x.p, nullptr, c.x.stride, 0, (u32)c.rows, c.n_in, ACT_NONE};
-        col_stats(x, c.type, nullptr, (float *)(c.ws + r.xc.inv), nullptr, s);
-        col_planes(d, dt, r.dc, c.ws, s);
-        col_planes(x, c.type, r.xc, c.ws, s);
+    if (dw) {
         const Planes &a = c.in_out ? r.xc : r.dc, &b = c.in_out ? r.dc : r.xc;
         Gemm g = {};
         g.M = c.in_out ? c.n_in : c.n_out;
