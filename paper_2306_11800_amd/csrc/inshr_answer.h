@@ -77,12 +77,7 @@ template <> struct Elem<TY_F32> {
 template <> struct Elem<TY_BF16> {
     typedef u16 type;
     static __device__ __forceinline__ float get(u16 v) { return __uint_as_float((u32)v << 16); }
-    static __device__ __forceinline__ u16 put(float v) // to nearest even, NaN stays NaN
-    {
-        const u32 b = __float_as_uint(v);
-        if ((b & 0x7fffffffu) > 0x7f800000u) return (u16)(b >> 16 | 0x40u);
-        return (u16)((b + 0x7fffu + (b >> 16 & 1u)) >> 16);
-    }
+    static __device__ __forceinline__ u16 put(float v) { return __builtin_bit_cast(u16, (__bf16)v); } // (to nearest even)
 };
 template <> struct Elem<TY_F16> {
     typedef _Float16 type;

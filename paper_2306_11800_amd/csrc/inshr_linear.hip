@@ -18,8 +18,19 @@ namespace inshr {
 // ------------------------------------------------------------------------------------------
 // planes of an operand whose reduction runs along its rows
 // ------------------------------------------------------------------------------------------
-constexpr u32 KT = 64;  // reduction per step of the product: planes are padded to it with zeros
+constexpr u32 KT = 64; // planes are padded to it along the reduction, with zeros
+constexpr u32 KS = 32; // reduction per step of the product
+constexpr u32 GROUP = 4;
 inline u64 up(u64 v, u64 to) { return (v + to - 1) / to * to; }
+
+// Planes lie in blocks of 16 rows x 32 numbers, 1024 bytes that one load of the product takes to LDS as they are: a row's
+// four pieces of eight numbers in an order of the row's own (piece c at c ^ (row / 4 % 4)), so that the 16 rows that a
+// read of LDS touches fall into different banks.  (Rows of a row-major plane gave the loads pieces of 64 bytes, at 60 % of
+// what a CU takes from L2 in whole lines.)  Place of number c of row r, for planes of ld numbers a row:
+__device__ __forceinline__ u64 plane_at(u64 r, u64 c, u64 ld)
+{
+    return ((r >> 4) * (ld / KS) + c / KS) * (16u * KS) + (r & 15u) * KS + ((c / 8u & 3u) ^ (r >> 2 & 3u)) * 8u + (c & 7u);
+}
 
 struct PlaneSrc { // a matrix of elements; act != ACT_NONE: multiplied by the slope at the values of `pre`
     const void *p, *pre;
@@ -88,7 +99,7 @@ __global__ __launch_bounds__(256) void k_row_planes(PlaneSrc src, _Float16 *__re
     for (u32 c = threadIdx.x * 8u; c < Cp; c += 2048u) {
         float v[8];
         load8<TY>(p + c, c < src.cols ? src.cols - c : 0u, v);
-        put_planes<P>(v, s, dst + r * Cp + c, plane);
+        put_planes<P>(v, s, dst + plane_at(r, c, Cp), plane);
     }
 }
 
@@ -104,7 +115,7 @@ struct TileJob {
     u32 *row_max, *col_max;  // [col_tiles][rows], [row_tiles][cols]; NULL: not wanted
     float *col_sum;          // [row_tiles][cols]
     float *inv_row, *inv_col, *sum; // joined
-    _Float16 *by_row, *by_col;      // planes [rows][ld_row], [cols][ld_col]
+    _Float16 *by_row, *by_col;      // planes of the rows, of the columns
     u64 plane_row, plane_col, ld_row, ld_col;
 };
 struct TileJobs {
@@ -126,8 +137,7 @@ __device__ __forceinline__ void tile_values(const PlaneSrc &src, u64 r0, u32 c0,
         if (src.act != ACT_NONE) {
             float a[8];
             load8<TY>((const GLOBAL_AS T *)src.pre + r * src.pre_stride + c, left, a);
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[h][i] = left ? v[h][i] * act_grad(a[i], src.act) : 0.0f;
+            act_grad(v[h], a, src.act); // (0 where nothing is: 0 times a slope at 0)
         }
     }
 }
@@ -237,7 +247,7 @@ __global__ __launch_bounds__(256) void k_tile_planes(TileJobs jobs)
 #pragma unroll
         for (u32 h = 0; h < 2u; h++) {
             const u64 r = r0 + (i >> 3) + 32u * h;
-            if (r < j.src.rows) put_planes<PR>(v[h], 1.0f / gptr(j.inv_row)[r], j.by_row + r * j.ld_row + c0 + (i & 7u) * 8u, j.plane_row);
+            if (r < j.src.rows) put_planes<PR>(v[h], 1.0f / gptr(j.inv_row)[r], j.by_row + plane_at(r, c0 + (i & 7u) * 8u, j.ld_row), j.plane_row);
         }
     }
     if (j.by_col) {
@@ -255,7 +265,7 @@ __global__ __launch_bounds__(256) void k_tile_planes(TileJobs jobs)
 #pragma unroll
             for (u32 q = 0; q < 8u; q++) x[q] = lds[r + q][c];
             const float s = 1.0f / gptr(j.inv_col)[c0 + c]; // (a power of two)
-            _Float16 *at = j.by_col + (u64)(c0 + c) * j.ld_col + r0 + r;
+            _Float16 *at = j.by_col + plane_at(c0 + c, r0 + r, j.ld_col);
             if (second)
                 put_planes<PC1>(x, s, at, j.plane_col);
             else
@@ -291,7 +301,7 @@ __device__ __forceinline__ void store_entries(const u32 (&e)[8][2], u32 skip, _F
 }
 constexpr u32 ONE_MARK = 0xFC00FC00u; // (minus infinity twice: no entry has a high part that is infinite and one that is left over)
 
-// Planes [rows][Cp] (T == false) or, turned, [cols][Rp]; padding of the reduction is zero.  A thread decodes runs of eight
+// Planes of the rows (T == false) or, turned, of the columns; padding of the reduction is zero.  A thread decodes runs of eight
 // symbols; protected places are left to the workgroups behind the tiles, which take them from the list (indices outside the
 // weight are left out).
 template <int W, int P, bool T>
@@ -308,7 +318,7 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
             if (r >= w.rows) continue;
             const float x = protected_value(w, j) * s;
             const _Float16 hi = (_Float16)x;
-            _Float16 *at = dst + (T ? (u64)c * ld + r : (u64)r * ld + c);
+            _Float16 *at = dst + (T ? plane_at(c, r, ld) : plane_at(r, c, ld));
             at[0] = hi;
             if (P > 1) at[plane] = (_Float16)(x - (float)hi);
         }
@@ -346,7 +356,7 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
 #pragma unroll
             for (int q = 0; q < 8; q++) turned[i / (TILE_C / 8u)][run * 8u + q] = symbol_of<W>(d, q) == 1u && (u32)q < left ? ONE_MARK : e[q][0];
         } else if (r < w.rows && c < (u32)ld) {
-            store_entries<P>(e, at_one, dst + r * ld + c, plane);
+            store_entries<P>(e, at_one, dst + plane_at(r, c, ld), plane);
         }
     }
     if (T) {
@@ -361,7 +371,7 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
                 e[q][0] = turned[r + q][c];
                 at_one |= (e[q][0] == ONE_MARK ? 1u : 0u) << q;
             }
-            store_entries<P>(e, at_one, dst + (u64)(c0 + c) * ld + r0 + r, plane);
+            store_entries<P>(e, at_one, dst + plane_at(c0 + c, r0 + r, ld), plane);
         }
     }
 }
@@ -370,7 +380,7 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
 // the product: C[m][n] = sum_k A[m][k] B[n][k], over pairs of planes
 // ------------------------------------------------------------------------------------------
 struct Gemm {
-    const _Float16 *a, *b;   // planes [M][ld], [N][ld]
+    const _Float16 *a, *b;   // planes of M and of N rows
     u64 plane_a, plane_b;
     u32 M, N, ld;            // ld: the padded reduction, of both
     u32 n_tiles, m_tiles;
@@ -380,7 +390,7 @@ struct Gemm {
     const u32 *wpart;
     Finish end;
     u32 type;                // of the results
-    u32 splits, steps;       // the reduction is dealt to `splits` workgroups, `steps` steps of KT each
+    u32 splits, steps;       // the reduction is dealt to `splits` workgroups, `steps` steps of KS each
     float *partial;          // [splits][M][n8] their sums; NULL: one workgroup has the whole reduction
     u32 n8;                  // N rounded up to 8
 };
@@ -403,15 +413,24 @@ __device__ __forceinline__ void scaled8(const Gemm &g, u32 m, u32 n, float (&v)[
     finish8<TY>(g.end, m, n, v);
 }
 
-// A tile of BM x BN, by waves of WM x WN.  A step takes 64 of the reduction: rows of 128 bytes in LDS, whose eight pieces
-// of 16 bytes lie in an order of the row's own (piece c at c ^ (row / 2 % 8)), so that the 16 rows that a read touches
-// fall into different banks.  The next step's rows are on their way while one is worked on.
-template <u32 TY, int BM, int BN, int WM, int WN>
+// Waits until at most N loads to LDS of this wave are on their way and all its reads of LDS have come, then for the others.
+template <int N>
+__device__ __forceinline__ void wait_and_meet()
+{
+    static_assert(N < 64, "");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// A tile of BM x BN, by waves of WM x WN.  A step takes 32 of the reduction: a block of the planes for 16 rows.  LDS holds D
+// steps.  While the matrix cores work on step t, the operands of step t + 1 are read from LDS into a second set of
+// registers, and the blocks of the steps up to t + D are on their way.
+template <u32 TY, int BM, int BN, int WM, int WN, int D>
 __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
 {
     constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TM = WM / 16, TN = WN / 16;
-    constexpr int LOADS = (BM + BN) / 8 / WAVES; // of 8 rows each, per wave and step
-    __shared__ __attribute__((aligned(1024))) _Float16 lds[2][(BM + BN) * KT];
+    constexpr int LOADS = (BM + BN) / 16 / WAVES; // of 16 rows each, per wave and step
+    constexpr u32 SLOT = (BM + BN) * KS;
+    __shared__ __attribute__((aligned(1024))) _Float16 lds[D * SLOT];
     const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
     // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles whose rows it finds in its own L2.
     u32 id = blockIdx.x;
@@ -420,50 +439,67 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
     const u32 per = (tiles + 7u) / 8u, full = tiles - (per - 1u) * 8u; // the first `full` XCDs have `per` tiles
     const u32 xcd = id & 7u, at = id >> 3;
     id = xcd < full ? xcd * per + at : full * per + (xcd - full) * (per - 1u) + at;
-    const u32 m0 = id % g.m_tiles * BM, n0 = id / g.m_tiles * BN;
+    // ... in strips of GROUP rows of tiles, so that a run is as high as it is wide
+    const u32 strip = id / (GROUP * g.n_tiles), in = id - strip * (GROUP * g.n_tiles), high = min(GROUP, g.m_tiles - strip * GROUP);
+    const u32 m0 = (strip * GROUP + in % high) * BM, n0 = in / high * BN;
     const u32 wm = wave % WAVES_M * WM, wn = wave / WAVES_M * WN;
-    // this lane's pieces of a step: row r of the tile's rows (a's, then b's)
+    // this wave's blocks of a step (a's, then b's)
     u64 from[LOADS];
     bool is_b[LOADS];
 #pragma unroll
     for (int j = 0; j < LOADS; j++) {
-        const u32 r = (wave * LOADS + j) * 8u + (lane >> 3), c = (lane & 7u) ^ ((r >> 1) & 7u);
-        is_b[j] = (wave * LOADS + j) * 8u >= (u32)BM;
-        // (rows past the last are the last: their results are not stored)
-        const u32 row = is_b[j] ? min(n0 + r - BM, g.N - 1u) : min(m0 + r, g.M - 1u);
-        from[j] = (u64)row * g.ld + c * 8u;
+        const u32 r = (wave * LOADS + j) * 16u;
+        is_b[j] = r >= (u32)BM;
+        // (blocks past the last are the last: their results are not stored)
+        const u32 block = is_b[j] ? min(n0 + r - BM, g.N - 1u) / 16u : min(m0 + r, g.M - 1u) / 16u;
+        from[j] = (u64)block * 16u * g.ld + lane * 8u;
     }
-    const u32 step0 = split * g.steps, n_steps = min(g.steps, g.ld / KT - step0) * g.pairs;
-    u32 k = step0 * KT, pass = 0;
-    auto fetch = [&](int buf) {
+    const u32 step0 = split * g.steps, n_steps = min(g.steps, g.ld / KS - step0) * g.pairs;
+    u64 k = step0 * (16u * KS); // blocks of a row follow each other
+    u32 pass = 0, asked = 0;
+    auto fetch = [&](u32 slot) { // the next step's rows; past the last step once more the last one's, which nobody reads
         const _Float16 *a = g.a + ((g.pa >> pass) & 1u) * g.plane_a + k, *b = g.b + ((g.pb >> pass) & 1u) * g.plane_b + k;
 #pragma unroll
-        for (int j = 0; j < LOADS; j++) to_lds((is_b[j] ? b : a) + from[j], lds[buf] + (wave * LOADS + j) * 8u * KT);
-        if (++pass == g.pairs) {
+        for (int j = 0; j < LOADS; j++) to_lds((is_b[j] ? b : a) + from[j], lds + slot * SLOT + (wave * LOADS + j) * (16u * KS));
+        if (++asked < n_steps && ++pass == g.pairs) {
             pass = 0;
-            k += KT;
+            k += 16u * KS;
         }
     };
+    struct Operands {
+        h8 a[TM], b[TN];
+    } even, odd;
+    const u32 r16 = lane & 15u, piece = ((lane >> 4) ^ (r16 >> 2)) * 8u;
+    auto read = [&](Operands &o, u32 slot) {
+        const _Float16 *as = lds + slot * SLOT + (wm + r16) * KS + piece, *bs = lds + slot * SLOT + (BM + wn + r16) * KS + piece;
+#pragma unroll
+        for (int j = 0; j < TN; j++) o.b[j] = *(const h8 *)(bs + j * 16 * KS);
+#pragma unroll
+        for (int i = 0; i < TM; i++) o.a[i] = *(const h8 *)(as + i * 16 * KS);
+    };
     f4 acc[TM][TN] = {};
-    fetch(0);
-    for (u32 t = 0; t < n_steps; t++) {
-        __syncthreads(); // this step's rows have come, and the other buffer has been read
-        if (t + 1 < n_steps) fetch((t + 1) & 1);
-        const _Float16 *as = lds[t & 1], *bs = as + BM * KT;
+    auto step = [&](const Operands &now, Operands &next, u32 t) {
+        wait_and_meet<LOADS *(D - 2)>(); // step t + 1 is there for all waves, and nobody reads step t any more
+        fetch(t % D);
+        read(next, (t + 1u) % D);
+        // (the columns of C are the rows of the instruction's result: a lane gets four consecutive ones)
 #pragma unroll
-        for (u32 kk = 0; kk < 2u; kk++) {
-            h8 fa[TM], fb[TN];
-            const u32 r = lane & 15u, c = ((kk * 4u + (lane >> 4)) ^ (r >> 1)) * 8u;
+        for (int i = 0; i < TM; i++)
 #pragma unroll
-            for (u32 i = 0; i < TM; i++) fa[i] = *(const h8 *)(as + (wm + i * 16u + r) * KT + c);
+            for (int j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.b[j], now.a[i], acc[i][j], 0, 0, 0);
 #pragma unroll
-            for (u32 j = 0; j < TN; j++) fb[j] = *(const h8 *)(bs + (wn + j * 16u + r) * KT + c);
-            // (the columns of C are the rows of the instruction's result: a lane gets four consecutive ones)
-#pragma unroll
-            for (u32 i = 0; i < TM; i++)
-#pragma unroll
-                for (u32 j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < TM + TN; i++) { // a few products, then a read
+            __builtin_amdgcn_sched_group_barrier(0x008, TM * TN / (TM + TN), 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+    };
+#pragma unroll
+    for (u32 q = 0; q < (u32)D; q++) fetch(q);
+    wait_and_meet<LOADS *(D - 1)>();
+    read(even, 0);
+    for (u32 t = 0; t < n_steps; t += 2u) {
+        step(even, odd, t);
+        if (t + 1u < n_steps) step(odd, even, t + 1u);
     }
     // The sums go through LDS, 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
     static_assert(WM % 64 == 0 && WN == 64, "");
@@ -548,7 +584,7 @@ Planes planes_for(Room &r, u64 rows, u64 reduction, u32 count)
 {
     Planes p;
     p.ld = up(reduction, KT);
-    p.plane = rows * p.ld;
+    p.plane = up(rows, 16) * p.ld;
     p.count = count;
     p.off = r.take(p.plane * count * 2u);
     p.inv = r.take(rows * 4u);
@@ -613,9 +649,9 @@ Cut cut_of(u64 M, u64 N, u64 ld)
     const u32 side = c.large ? 256u : 128u;
     c.m_tiles = (u32)((M + side - 1) / side);
     c.n_tiles = (u32)((N + side - 1) / side);
-    const u64 tiles = (u64)c.m_tiles * c.n_tiles, steps = ld / KT;
+    const u64 tiles = (u64)c.m_tiles * c.n_tiles, steps = ld / KS;
     c.splits = 1;
-    while (!c.large && c.splits < 8u && tiles * c.splits < CUS && steps / (2u * c.splits) >= 4u) c.splits *= 2u;
+    while (!c.large && c.splits < 8u && tiles * c.splits < CUS && steps / (2u * c.splits) >= 8u) c.splits *= 2u;
     c.steps = (u32)((steps + c.splits - 1) / c.splits);
     c.splits = (u32)((steps + c.steps - 1) / c.steps); // (none without a step)
     c.partial = c.splits > 1 ? up(N, 8) * M * c.splits * 4u : 0;
@@ -627,9 +663,9 @@ void product_of(const Gemm &g, const Cut &c, hipStream_t s)
 {
     const u32 grid = c.m_tiles * c.n_tiles * c.splits;
     if (c.large)
-        PROF("k_product", s, k_product<TY, 256, 256, 128, 64><<<grid, 512, 0, s>>>(g));
+        PROF("k_product", s, k_product<TY, 256, 256, 128, 64, 4><<<grid, 512, 0, s>>>(g));
     else
-        PROF("k_product", s, k_product<TY, 128, 128, 64, 64><<<grid, 256, 0, s>>>(g));
+        PROF("k_product", s, k_product<TY, 128, 128, 64, 64, 8><<<grid, 256, 0, s>>>(g));
     if (c.splits > 1) {
         const u64 all = (u64)g.M * (g.n8 / 8u), blocks = (all + 255) / 256;
         PROF("k_join", s, k_join<TY><<<(u32)(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(g));
