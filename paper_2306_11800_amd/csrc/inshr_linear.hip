@@ -209,7 +209,7 @@ __global__ __launch_bounds__(256) void k_scales(TileJobs jobs)
         if (i < j.src.rows) {
             if (!j.row_max) return;
             u32 m = 0u;
-#pragma unroll 4
+#pragma unroll 16
             for (u32 t = 0; t < j.col_tiles; t++) m = max(m, gptr(j.row_max)[(u64)t * j.src.rows + i]);
             float s;
             scale_of(m, s, j.inv_row[i]);
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256) void k_scales(TileJobs jobs)
         if (i < j.src.cols) {
             u32 m = 0u;
             float sum = 0.0f, s;
-#pragma unroll 4
+#pragma unroll 8
             for (u32 t = 0; t < j.row_tiles; t++) {
                 if (j.col_max) m = max(m, gptr(j.col_max)[(u64)t * j.src.cols + i]);
                 if (j.col_sum) sum += gptr(j.col_sum)[(u64)t * j.src.cols + i];
@@ -395,10 +395,10 @@ struct Gemm {
     u32 n8;                  // N rounded up to 8
 };
 
-// 16 bytes per lane from device memory to LDS without registers in between: lane l's go to `to` + 16 l.
-__device__ __forceinline__ void to_lds(const _Float16 *from, _Float16 *to)
+// A block of 1024 bytes from device memory to LDS without registers in between.
+__device__ __forceinline__ void to_lds(const _Float16 *from, u32 lane, _Float16 *to)
 {
-    __builtin_amdgcn_global_load_lds((const GLOBAL_AS u32 *)from, (LDS_AS u32 *)to, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const GLOBAL_AS u32 *)from + lane * 4u, (LDS_AS u32 *)to, 16, 0, 0);
 }
 
 // The scaled sums of row m, columns n .. n + 7, to where they belong.
@@ -425,20 +425,23 @@ __device__ __forceinline__ void wait_and_meet()
 // steps.  While the matrix cores work on step t, the operands of step t + 1 are read from LDS into a second set of
 // registers, and the blocks of the steps up to t + D are on their way.
 template <u32 TY, int BM, int BN, int WM, int WN, int D>
+// (Eight waves: with four, one a SIMD, the compiler keeps the sums in accumulation registers and moves them to and fro
+// around every product, 0.5 us a step of 128 x 128.)
 __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
 {
     constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TM = WM / 16, TN = WN / 16;
     constexpr int LOADS = (BM + BN) / 16 / WAVES; // of 16 rows each, per wave and step
     constexpr u32 SLOT = (BM + BN) * KS;
     __shared__ __attribute__((aligned(1024))) _Float16 lds[D * SLOT];
-    const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
-    // Workgroups go to the eight XCDs in turn; each XCD gets a run of tiles whose rows it finds in its own L2.
-    u32 id = blockIdx.x;
-    const u32 tiles = g.m_tiles * g.n_tiles, split = id / tiles;
+    // (the wave's number in a scalar register, and with it all addresses but the lane's 16 bytes)
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
+    // Workgroups go to the eight XCDs in turn; each XCD gets a run of them, of one split first, whose blocks it finds in its
+    // own L2 ...
+    const u32 tiles = g.m_tiles * g.n_tiles, all = tiles * g.splits, per = (all + 7u) / 8u;
+    const u32 full = all - (per - 1u) * 8u, xcd = blockIdx.x & 7u, at = blockIdx.x >> 3; // the first `full` XCDs have `per`
+    u32 id = xcd < full ? xcd * per + at : full * per + (xcd - full) * (per - 1u) + at;
+    const u32 split = id / tiles;
     id -= split * tiles;
-    const u32 per = (tiles + 7u) / 8u, full = tiles - (per - 1u) * 8u; // the first `full` XCDs have `per` tiles
-    const u32 xcd = id & 7u, at = id >> 3;
-    id = xcd < full ? xcd * per + at : full * per + (xcd - full) * (per - 1u) + at;
     // ... in strips of GROUP rows of tiles, so that a run is as high as it is wide
     const u32 strip = id / (GROUP * g.n_tiles), in = id - strip * (GROUP * g.n_tiles), high = min(GROUP, g.m_tiles - strip * GROUP);
     const u32 m0 = (strip * GROUP + in % high) * BM, n0 = in / high * BN;
@@ -452,7 +455,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
         is_b[j] = r >= (u32)BM;
         // (blocks past the last are the last: their results are not stored)
         const u32 block = is_b[j] ? min(n0 + r - BM, g.N - 1u) / 16u : min(m0 + r, g.M - 1u) / 16u;
-        from[j] = (u64)block * 16u * g.ld + lane * 8u;
+        from[j] = (u64)block * 16u * g.ld;
     }
     const u32 step0 = split * g.steps, n_steps = min(g.steps, g.ld / KS - step0) * g.pairs;
     u64 k = step0 * (16u * KS); // blocks of a row follow each other
@@ -460,7 +463,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
     auto fetch = [&](u32 slot) { // the next step's rows; past the last step once more the last one's, which nobody reads
         const _Float16 *a = g.a + ((g.pa >> pass) & 1u) * g.plane_a + k, *b = g.b + ((g.pb >> pass) & 1u) * g.plane_b + k;
 #pragma unroll
-        for (int j = 0; j < LOADS; j++) to_lds((is_b[j] ? b : a) + from[j], lds + slot * SLOT + (wave * LOADS + j) * (16u * KS));
+        for (int j = 0; j < LOADS; j++) to_lds((is_b[j] ? b : a) + from[j], lane, lds + slot * SLOT + (wave * LOADS + j) * (16u * KS));
         if (++asked < n_steps && ++pass == g.pairs) {
             pass = 0;
             k += 16u * KS;
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
             for (int j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.b[j], now.a[i], acc[i][j], 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < TM + TN; i++) { // a few products, then a read
-            __builtin_amdgcn_sched_group_barrier(0x008, TM * TN / (TM + TN), 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, (TM * TN + TM + TN - 1) / (TM + TN), 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
     };
@@ -501,35 +504,32 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
         step(even, odd, t);
         if (t + 1u < n_steps) step(odd, even, t + 1u);
     }
-    // The sums go through LDS, 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
-    static_assert(WM % 64 == 0 && WN == 64, "");
+    // The sums go through LDS, up to 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
+    static_assert(WN == 64, "");
+    constexpr int ROWS = WM < 64 ? WM : 64;
     float s, inv_w = 1.0f;
     if (!g.inv_b && !g.partial) weight_scale(g.wpart, s, inv_w);
-    float *const mine = (float *)lds + wave * 4096u; // [64][64], the pieces of 4 of a row in an order of its own
+    float *const mine = (float *)lds + wave * (ROWS * 64u); // [ROWS][64], the pieces of 4 of a row in an order of its own
+    const u32 n = n0 + wn + (lane & 7u) * 8u;
 #pragma unroll
-    for (int half = 0; half < WM / 64; half++) {
+    for (int part = 0; part < WM / ROWS; part++) {
         __syncthreads();
 #pragma unroll
-        for (u32 i = 0; i < 4u; i++)
+        for (u32 i = 0; i < ROWS / 16u; i++)
 #pragma unroll
-            for (u32 j = 0; j < 4u; j++) {
-                const u32 r = lane & 15u, c = j * 4u + (lane >> 4);
-                *(f4 *)(mine + (i * 16u + r) * 64u + ((c ^ r) * 4u)) = acc[half * 4 + i][j];
-            }
+            for (u32 j = 0; j < 4u; j++) *(f4 *)(mine + (i * 16u + r16) * 64u + ((j * 4u + (lane >> 4)) ^ r16) * 4u) = acc[part * (ROWS / 16) + i][j];
         __syncthreads();
-        const u32 n = n0 + wn + (lane & 7u) * 8u;
 #pragma unroll 1
-        for (u32 q = 0; q < 8u; q++) {
-            const u32 r = q * 8u + (lane >> 3), m = m0 + wm + half * 64u + r, c = (lane & 7u) * 2u;
+        for (u32 q = 0; q < ROWS / 8u; q++) {
+            const u32 r = q * 8u + (lane >> 3), m = m0 + wm + part * ROWS + r, c = (lane & 7u) * 2u;
             if (m >= g.M || n >= g.N) continue;
-            float v[8];
-            *(f4 *)v = *(const f4 *)(mine + r * 64u + (c ^ (r & 15u)) * 4u);
-            *(f4 *)(v + 4) = *(const f4 *)(mine + r * 64u + ((c + 1u) ^ (r & 15u)) * 4u);
+            const f4 x = *(const f4 *)(mine + r * 64u + (c ^ (r & 15u)) * 4u), y = *(const f4 *)(mine + r * 64u + ((c + 1u) ^ (r & 15u)) * 4u);
             if (g.partial) {
                 float *to = g.partial + ((u64)split * g.M + m) * g.n8 + n;
-                *(f4 *)to = *(const f4 *)v;
-                *(f4 *)(to + 4) = *(const f4 *)(v + 4);
+                *(f4 *)to = x;
+                *(f4 *)(to + 4) = y;
             } else {
+                float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
                 scaled8<TY>(g, m, n, v, inv_w);
             }
         }
@@ -634,24 +634,33 @@ void weight_planes(const WDesc &w, bool along, const Planes &p, char *ws, u64 pa
     });
 }
 
-// How a product is cut: tiles of 256 x 256 or 128 x 128, and the reduction among several workgroups where there are few tiles.
+// How a product is cut: tiles of 256 x 256, 128 x 256 or 128 x 128, whichever rounds of 256 workgroups take the least time
+// (a step of a tile measured 0.91, 0.52 and 0.30 us on a full chip), and with tiles too few for the chip the reduction
+// among several workgroups.
 struct Cut {
-    bool large;
+    int kind;
     u32 m_tiles, n_tiles, splits, steps;
     u64 partial; // bytes
 };
 constexpr u32 CUS = 256;
-Cut cut_of(u64 M, u64 N, u64 ld)
+constexpr u32 KIND_M[3] = {256, 128, 128}, KIND_N[3] = {256, 256, 128}, KIND_TIME[3] = {91, 52, 30};
+Cut cut_of(u64 M, u64 N, u64 ld, u32 pairs)
 {
     Cut c;
-    const u64 big = up(M, 256) / 256 * (up(N, 256) / 256);
-    c.large = big >= CUS;
-    const u32 side = c.large ? 256u : 128u;
-    c.m_tiles = (u32)((M + side - 1) / side);
-    c.n_tiles = (u32)((N + side - 1) / side);
+    u64 best = ~0ull;
+    for (int kind = 0; kind < 3; kind++) {
+        const u64 tiles = up(M, KIND_M[kind]) / KIND_M[kind] * (up(N, KIND_N[kind]) / KIND_N[kind]);
+        const u64 time = up(tiles, CUS) / CUS * KIND_TIME[kind];
+        if (time < best) {
+            best = time;
+            c.kind = kind;
+        }
+    }
+    c.m_tiles = (u32)(up(M, KIND_M[c.kind]) / KIND_M[c.kind]);
+    c.n_tiles = (u32)(up(N, KIND_N[c.kind]) / KIND_N[c.kind]);
     const u64 tiles = (u64)c.m_tiles * c.n_tiles, steps = ld / KS;
     c.splits = 1;
-    while (!c.large && c.splits < 8u && tiles * c.splits < CUS && steps / (2u * c.splits) >= 8u) c.splits *= 2u;
+    while (c.splits < 16u && tiles * c.splits * 2u <= CUS && steps * pairs / (2u * c.splits) >= 8u && steps >= 2u * c.splits) c.splits *= 2u;
     c.steps = (u32)((steps + c.splits - 1) / c.splits);
     c.splits = (u32)((steps + c.steps - 1) / c.steps); // (none without a step)
     c.partial = c.splits > 1 ? up(N, 8) * M * c.splits * 4u : 0;
@@ -662,10 +671,11 @@ template <u32 TY>
 void product_of(const Gemm &g, const Cut &c, hipStream_t s)
 {
     const u32 grid = c.m_tiles * c.n_tiles * c.splits;
-    if (c.large)
-        PROF("k_product", s, k_product<TY, 256, 256, 128, 64, 4><<<grid, 512, 0, s>>>(g));
-    else
-        PROF("k_product", s, k_product<TY, 128, 128, 64, 64, 8><<<grid, 256, 0, s>>>(g));
+    switch (c.kind) {
+    case 0: PROF("k_product", s, k_product<TY, 256, 256, 128, 64, 4><<<grid, 512, 0, s>>>(g)); break;
+    case 1: PROF("k_product", s, k_product<TY, 128, 256, 64, 64, 4><<<grid, 512, 0, s>>>(g)); break;
+    default: PROF("k_product", s, k_product<TY, 128, 128, 32, 64, 8><<<grid, 512, 0, s>>>(g)); break;
+    }
     if (c.splits > 1) {
         const u64 all = (u64)g.M * (g.n8 / 8u), blocks = (all + 255) / 256;
         PROF("k_join", s, k_join<TY><<<(u32)(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(g));
@@ -685,7 +695,7 @@ void product(Gemm g, const Planes &a, const Planes &b, u64 partial, char *ws, hi
     if (a.count > 1) g.pa |= 1u << g.pairs++;
     if (b.count > 1) g.pb |= 1u << g.pairs++;
     g.pairs++;
-    const Cut c = cut_of(g.M, g.N, a.ld);
+    const Cut c = cut_of(g.M, g.N, a.ld, g.pairs);
     g.m_tiles = c.m_tiles;
     g.n_tiles = c.n_tiles;
     g.splits = c.splits;
@@ -712,7 +722,7 @@ struct LinearRoom {
         x = planes_for(r, rows, n_in, planes_x(type));
         w = planes_for(r, n_out, n_in, planes_w(type));
         part = r.take(WMAX_PARTS * 4u);
-        partial = r.take(cut_of(rows, n_out, x.ld).partial);
+        partial = r.take(cut_of(rows, n_out, x.ld, x.count + w.count - 1).partial);
         bytes = r.at;
     }
 };
@@ -740,8 +750,8 @@ struct GradRoom {
             x_max = r.take(row_tiles * n_in * 4u);
         }
         // (the two products take turns)
-        u64 most = dx ? cut_of(rows, n_in, dr.ld).partial : 0;
-        if (dw) most = std::max(most, std::max(cut_of(n_out, n_in, dc.ld).partial, cut_of(n_in, n_out, dc.ld).partial));
+        u64 most = dx ? cut_of(rows, n_in, dr.ld, dr.count + w.count - 1).partial : 0;
+        if (dw) most = std::max(most, std::max(cut_of(n_out, n_in, dc.ld, dc.count + xc.count - 1).partial, cut_of(n_in, n_out, dc.ld, dc.count + xc.count - 1).partial));
         partial = r.take(most);
         bytes = r.at;
     }
