@@ -42,12 +42,14 @@ struct LinearGradCall {
     u32 n_in, n_out, in_out, type, act;
     char *ws;                // workspace, linear_grad_space() bytes
 };
-u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type);
+u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, bool listed);
 u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw);
 hipError_t launch_linear(const LinearCall &c, hipStream_t s);
-hipError_t launch_few(const LinearCall &c, hipStream_t s); // few rows: no workspace
-// FEWRULE
-inline bool is_few(u64 rows) { return rows <= 64; }
+// Few rows: straight from the stream.
+constexpr u32 FEW_ROWS = 64, FEW_SPLIT = 4;
+inline bool is_few(u64 rows, bool in_out) { return rows <= (in_out ? FEW_SPLIT : FEW_ROWS); }
+u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed);
+hipError_t launch_few(const LinearCall &c, hipStream_t s);
 hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s);
 
 constexpr u32 MAX_VOCAB = 1u << 18; // a bit per logit of a row fits into 32 KB of LDS

@@ -2488,7 +2488,7 @@ int inshr_linear_bound(const inshr_layer *layer, uint64_t rows, uint64_t *worksp
     WDesc w;
     const int rc = layer_of(layer, rows, w);
     if (rc) return rc;
-    *workspace_bytes = linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type);
+    *workspace_bytes = linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->weight.n_outlier != 0);
     return INSHR_OK;
 }
 
@@ -2506,7 +2506,7 @@ int inshr_linear(inshr_ctx *c, const inshr_layer *layer, inshr_matrix x, inshr_m
         return INSHR_E_ARG;
     if (residual.data == y.data && residual.stride != y.stride) return INSHR_E_ARG;
     rc = workspace_ok(c, "inshr_linear", workspace, workspace_bytes,
-                      linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type));
+                      linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->weight.n_outlier != 0));
     if (rc) return rc;
     call.bias = layer->bias;
     call.x = mat(x);

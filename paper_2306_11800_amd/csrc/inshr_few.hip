@@ -1,22 +1,21 @@
 // Products of a few rows with a weight in its compressed form: the symbols go from the stream through a table in LDS
-// straight into the operands of the matrix cores.
+// straight into the operands.
 //
 // What bounds it: the stream (w / 8 bytes a weight) and the vector instructions that take the symbols apart (two to place
-// a symbol as a table address, one to put its value next to its neighbour's; the table look-up runs beside them).  The
-// matrix cores have time to spare, so the factors keep all their bits:
-//   bfloat16  the centre as two bfloat16 numbers (16 bits), two instructions
-//   fp16      the centre scaled by a power of two as two fp16 numbers (22 bits), two instructions
-//   fp32      centre and activation as three bfloat16 numbers each (all 24 bits), the six products that matter
-//
-// A lane decodes whole runs of consecutive symbols, so that after one funnel shift to the run's first bit all positions
-// are constants.  Which k's of the reduction meet in an instruction is free as long as both operands agree:
-//   weight [n_out][n_in]  (k_few_rows)  lane (i, g) takes 32 consecutive k of output i, 8 of them per instruction
-//   weight [n_in][n_out]  (k_few_cols)  lane (i, g) takes R consecutive outputs of 8 consecutive k; the t-th of them go
-//                                        into instruction t, whose outputs are then R apart
-// A workgroup's waves share its outputs and split the reduction; their sums are joined in a fixed order.
-//
-// Protected values are 0 in the table and are added at the end, from the list, in fixed point: whole numbers add up to
-// the same sum in any order.
+// a symbol as a table address, one to put its value next to its neighbour's or to multiply it; the table look-up runs beside
+// them).  A lane decodes whole runs of consecutive symbols, so that after one funnel shift to the run's first bit all
+// positions are constants.
+//   weight [n_out][n_in]  k_few_rows: the reduction runs along the stream.  Lane (i, g) takes 32 consecutive k of output i, 8 of
+//                         them per instruction of the matrix cores (which k's meet in an instruction is free as long as both
+//                         operands agree).  The matrix cores have time to spare, so the factors keep all their bits:
+//                           bfloat16  the centre as two bfloat16 numbers (16 bits), two instructions
+//                           fp16      the centre scaled by a power of two as two fp16 numbers (22 bits), two instructions
+//                           fp32      centre and activation as three bfloat16 numbers each (all 24 bits), the six products
+//                                     that matter
+//   weight [n_in][n_out]  k_few_split: a thread keeps the sums of 8 consecutive outputs and walks down a part of the rows of
+//                         the weight; k_few_join adds the parts.  fp32 throughout, one multiplication per weight and row of
+//                         activations, which is why it takes up to FEW_SPLIT rows.
+// All sums are taken in a fixed order.  Protected values are 0 in the table and are added from the list.
 #include "inshr_table.h"
 
 namespace inshr {
@@ -95,6 +94,14 @@ __device__ __forceinline__ f4 multiply(const Parts<TY> &w, const Xs<TY> &x, f4 c
     }
 }
 
+// The scale of the centres alone, by every wave.
+__device__ __forceinline__ void centre_scale(const WDesc &w, float &s, float &inv)
+{
+    u32 m = 0u;
+    for (u32 i = threadIdx.x & 63u; i < w.K; i += 64u) m = max(m, finite_mag(gptr(w.codebook)[i]));
+    scale_of(wave_max_u(m), s, inv);
+}
+
 // ------------------------------------------------------------------------------------------
 // protected values
 // ------------------------------------------------------------------------------------------
@@ -113,131 +120,85 @@ __device__ __forceinline__ u64 first_listed(const WDesc &w, u64 index, u32 half_
     return lo;
 }
 
-struct Few {
-    WDesc w;
-    Finish end;
-    Mat x;
-    u32 rows, n_in, n_out, in_out;
-    u32 cols;        // outputs of a workgroup
-    u32 row_blocks;  // blocks of 16 MT rows
-    u32 sums_at;     // byte offsets into LDS: the joined sums, ...
-    u32 listed_at;   // ... the protected values' part of them
-};
-
-// The scale of the centres alone, by every wave.
-__device__ __forceinline__ void centre_scale(const WDesc &w, float &s, float &inv)
+// Where the entries of each stored row begin: starts[t] for rows r0 + t, t = 0 .. n, relative to lo.  lo .. hi: the entries of
+// these rows.  By the whole workgroup; a barrier has to follow.  (A list that is not in order may leave places unset: they
+// are read as at most hi - lo.)
+__device__ __forceinline__ void row_starts(const WDesc &w, u64 lo, u64 hi, u32 r0, u32 n, u32 *starts)
 {
-    u32 m = 0u;
-    for (u32 i = threadIdx.x & 63u; i < w.K; i += 64u) m = max(m, finite_mag(gptr(w.codebook)[i]));
-    scale_of(wave_max_u(m), s, inv);
-}
-
-// The joined sums of a workgroup, cols of them per row, lie at `sums`; adds the protected values' part and stores the
-// results.  lo .. hi: the entries of the list that may belong to the workgroup.
-template <u32 TY, int MT>
-__device__ void finish(const Few &f, char *lds, u64 lo, u64 hi, u32 m0, u32 n0, float inv)
-{
-    typedef typename Elem<TY>::type T;
-    const float *sums = (const float *)(lds + f.sums_at);
-    unsigned long long *listed = (unsigned long long *)(lds + f.listed_at);
-    __shared__ u32 high[16 * MT]; // largest magnitude of a row's products
-    const u32 rows = min(f.rows - m0, 16u * MT), cells = rows * f.cols;
-    const bool any = hi > lo;
-    if (any) {
-        // Fixed point: the largest magnitude of a product of the row gets 40 bits, so that nothing is off by more than
-        // 2^-41 of it (and 2^22 of them still fit).
-        if (threadIdx.x < 16u * MT) high[threadIdx.x] = 0u;
-        for (u32 i = threadIdx.x; i < cells; i += blockDim.x) listed[i] = 0ull;
-        __syncthreads();
-        u32 m_high[16 * MT];
-#pragma unroll
-        for (int m = 0; m < 16 * MT; m++) m_high[m] = 0u;
-        for (int pass = 0; pass < 2; pass++) {
-            for (u64 j = lo + threadIdx.x; j < hi; j += blockDim.x) {
-                const u32 at = gptr(f.w.out_idx)[j], r = at / f.w.cols, c = at - r * f.w.cols;
-                const u32 n = f.in_out ? c : r, k = f.in_out ? r : c;
-                if (r >= f.w.rows || n < n0 || n >= n0 + f.cols) continue;
-                const float v = protected_value(f.w, j);
-                const GLOBAL_AS T *x = (const GLOBAL_AS T *)f.x.p + (u64)m0 * f.x.stride + k;
-#pragma unroll
-                for (u32 m = 0; m < 16u * MT; m++) {
-                    if (m >= rows) continue;
-                    const float p = v * Elem<TY>::get(x[(u64)m * f.x.stride]);
-                    if (pass == 0)
-                        m_high[m] = max(m_high[m], finite_mag(p));
-                    else if (mag_bits(p) < 0x7f800000u) // a product below 2^(e - 126) times this is below 2^40
-                        atomicAdd(&listed[m * f.cols + n - n0],
-                                  (unsigned long long)__double2ll_rn(ldexp((double)p, 166 - (int)(high[m] >> 23))));
-                }
-            }
-            if (pass == 0) {
-#pragma unroll
-                for (u32 m = 0; m < 16u * MT; m++) {
-                    if (m >= rows) continue;
-                    const u32 w = wave_max_u(m_high[m]);
-                    if ((threadIdx.x & 63u) == 0u) atomicMax(&high[m], w);
-                }
-            }
-            __syncthreads();
-        }
-    }
-    for (u32 i = threadIdx.x; i < cells / 8u; i += blockDim.x) {
-        const u32 m = i / (f.cols / 8u), n = (i - m * (f.cols / 8u)) * 8u;
-        if (n0 + n >= f.n_out) continue;
-        float v[8];
-#pragma unroll
-        for (u32 t = 0; t < 8u; t++) {
-            v[t] = sums[m * f.cols + n + t] * inv;
-            if (any) v[t] += (float)ldexp((double)(long long)listed[m * f.cols + n + t], (int)(high[m] >> 23) - 166);
-        }
-        finish8<TY>(f.end, m0 + m, n0 + n, v);
+    const u32 count = (u32)(hi - lo);
+    for (u32 j = threadIdx.x; j <= count; j += blockDim.x) {
+        // (clamped: a list that is not in order must not lead out of the array)
+        const u32 before = j == 0u ? 0u : min(gptr(w.out_idx)[lo + j - 1u] / w.cols - r0 + 1u, n + 1u);
+        const u32 here = j == count ? n : min(gptr(w.out_idx)[lo + j] / w.cols - r0, n);
+        for (u32 t = before; t <= here; t++) starts[t] = j;
     }
 }
 
 // ------------------------------------------------------------------------------------------
 // weight [n_out][n_in]
 // ------------------------------------------------------------------------------------------
-// 16 outputs, 16 MT rows; the last wave looks the workgroup's part of the protected list up while the others work.
-template <u32 TY, int W, int MT>
-__global__ __launch_bounds__(1024) void k_few_rows(Few f)
+constexpr u32 TURNED = 32; // rows of activations side by side in their turned copy
+constexpr u32 FEW_TURNED = 4; // up to as many rows the protected values' activations are taken from the rows themselves
+
+struct Few {
+    WDesc w;
+    Finish end;
+    Mat x;
+    const void *turned; // [row blocks of TURNED][n_in][TURNED] activations, or NULL
+    float *partial;     // k_few_split: [splits][rows][n8]
+    u32 rows, n_in, n_out, n8;
+    u32 row_blocks;     // blocks of 16 MT rows
+    u32 splits, depth;  // k_few_split: parts of the reduction, rows of a part
+};
+
+// x turned: blocks of TURNED rows, so that the activations that a protected value meets lie side by side.
+template <u32 TY>
+__global__ __launch_bounds__(256) void k_few_turn(Mat x, u32 rows, u32 cols, typename Elem<TY>::type *__restrict__ to)
 {
     typedef typename Elem<TY>::type T;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ u64 range[2];
-    u32 *table = (u32 *)lds;
-    f4 *part = (f4 *)(lds + Table<TY, W>::BYTES);
-    const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, waves = (blockDim.x >> 6) - 1u;
-    const u32 n0 = blockIdx.x / f.row_blocks * 16u, m0 = blockIdx.x % f.row_blocks * (16u * MT);
-    float s = 1.0f, inv = 1.0f;
-    if (TY == TY_F16) centre_scale(f.w, s, inv);
-    fill_table<TY, W>(f.w, table, s);
+    __shared__ T tile[64][TURNED + 2];
+    const u32 c0 = blockIdx.x * 64u, r0 = blockIdx.y * TURNED;
+    for (u32 i = threadIdx.x; i < 64u * TURNED; i += 256u) {
+        const u32 r = r0 + i / 64u, c = c0 + i % 64u;
+        tile[i % 64u][i / 64u] = r < rows && c < cols ? ((const GLOBAL_AS T *)x.p)[(u64)r * x.stride + c] : (T)0;
+    }
     __syncthreads();
-    f4 acc[MT] = {};
-    if (wave == waves) {
-        const u32 half = lane >> 5;
-        const u64 first = (u64)min(n0 + half * 16u, f.n_out) * f.n_in;
-        const u64 at = f.w.n_outlier ? first_listed(f.w, first, lane & 31u, half) : 0;
-        if ((lane & 31u) == 0u) range[half] = at;
-    } else {
-        const u32 i = lane & 15u, g = lane >> 4, K = f.n_in;
-        const u64 row_bit = (u64)min(n0 + i, f.n_out - 1u) * K * W;
-        const u32 mine = lane_copy<TY, W>();
-        const GLOBAL_AS T *x[MT];
+    for (u32 i = threadIdx.x; i < 64u * TURNED; i += 256u) {
+        const u32 c = i / TURNED;
+        if (c0 + c < cols) to[((u64)blockIdx.y * cols + c0 + c) * TURNED + i % TURNED] = tile[c][i % TURNED];
+    }
+}
+
+constexpr u32 AHEAD = 2; // steps whose part of the stream is asked for before one is worked on
+
+// This wave's steps of 128 of the reduction, `every` apart.  SAFE: no load of the stream can lead past its end.
+template <u32 TY, int W, int MT, bool SAFE>
+__device__ __forceinline__ void few_steps(const Few &f, const char *table, u32 n0, u32 m0, u32 k0, u32 every, u32 (&raw)[AHEAD][W + 1], f4 (&acc)[MT])
+{
+    typedef typename Elem<TY>::type T;
+    const u32 lane = threadIdx.x & 63u, i = lane & 15u, g = lane >> 4, K = f.n_in;
+    const u64 row_bit = (u64)min(n0 + i, f.n_out - 1u) * K * W;
+    const u32 mine = lane_copy<TY, W>();
+    const GLOBAL_AS T *x[MT];
 #pragma unroll
-        for (int t = 0; t < MT; t++) {
-            x[t] = (const GLOBAL_AS T *)f.x.p + (u64)min(m0 + 16u * t + i, f.rows - 1u) * f.x.stride;
-        }
-        for (u32 k0 = wave * 128u; k0 < K; k0 += waves * 128u) {
-            const u32 k = k0 + 32u * g, left = k < K ? K - k : 0u;
-            u32 raw[W + 1], d[W];
-            const u64 bit = row_bit + (u64)k * W;
-            load_words<W + 1>(f.w.packed, bit >> 5, left ? f.w.n_words : 0, raw);
+    for (int t = 0; t < MT; t++) x[t] = (const GLOBAL_AS T *)f.x.p + (u64)min(m0 + 16u * t + i, f.rows - 1u) * f.x.stride;
+    for (; k0 < K; k0 += AHEAD * every) {
 #pragma unroll
-            for (int j = 0; j < W; j++) d[j] = __builtin_amdgcn_alignbit(raw[j + 1], raw[j], (u32)bit & 31u);
-            if (left < 32u) { // what follows in the stream is another output's
+        for (u32 ahead = 0; ahead < AHEAD; ahead++) {
+            const u32 kb = k0 + ahead * every, k = kb + 32u * g;
+            if (kb >= K) break;
+            const u32 left = k < K ? K - k : 0u;
+            const bool full = kb + 128u <= K; // (the same for all lanes)
+            u32 d[W];
+            const u32 shift = (u32)(row_bit + (u64)k * W) & 31u;
+#pragma unroll
+            for (int j = 0; j < W; j++) d[j] = __builtin_amdgcn_alignbit(raw[ahead][j + 1], raw[ahead][j], shift);
+            const u32 next = k + AHEAD * every;
+            if (kb + AHEAD * every < K) load_words<W + 1, SAFE>(f.w.packed, (row_bit + (u64)next * W) >> 5, next < K ? f.w.n_words : 0, raw[ahead]);
+            if (kb + 128u > K) { // what follows in the stream is another output's
 #pragma unroll
                 for (int j = 0; j < W; j++) {
-                    const int keep = (int)(left * W) - 32 * j;
+                    const int keep = (int)(min(left, 32u) * W) - 32 * j;
                     d[j] = keep >= 32 ? d[j] : keep <= 0 ? 0u : d[j] & ((1u << keep) - 1u);
                 }
             }
@@ -247,103 +208,260 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     u32 a[2], b[2];
-                    look_up<TY, W>((const char *)table, mine, d, 8 * s + 2 * j, a);
-                    look_up<TY, W>((const char *)table, mine, d, 8 * s + 2 * j + 1, b);
+                    look_up<TY, W>(table, mine, d, 8 * s + 2 * j, a);
+                    look_up<TY, W>(table, mine, d, 8 * s + 2 * j + 1, b);
                     put_entries<TY>(w, j, a, b);
                 }
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
                     Xs<TY> v;
-                    load_xs<TY>(x[t] + k + 8 * s, left > 8u * s ? left - 8u * s : 0u, v);
+                    load_xs<TY>(x[t] + k + 8u * s, full ? 8u : left > 8u * s ? left - 8u * s : 0u, v);
                     acc[t] = multiply<TY>(w, v, acc[t]);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0); // (one step's activations in registers at a time)
         }
+    }
+}
+// The stream of the first AHEAD steps: asked for before anything else.
+template <int W, bool SAFE>
+__device__ __forceinline__ void few_first(const Few &f, u32 n0, u32 k0, u32 every, u32 (&raw)[AHEAD][W + 1])
+{
+    const u32 lane = threadIdx.x & 63u, K = f.n_in;
+    const u64 row_bit = (u64)min(n0 + (lane & 15u), f.n_out - 1u) * K * W;
+#pragma unroll
+    for (u32 ahead = 0; ahead < AHEAD; ahead++) {
+        const u32 kb = k0 + ahead * every, k = kb + 32u * (lane >> 4);
+        if (kb < K) load_words<W + 1, SAFE>(f.w.packed, (row_bit + (u64)k * W) >> 5, k < K ? f.w.n_words : 0, raw[ahead]);
+    }
+}
+
+// 16 outputs, 16 MT rows; the last wave looks the workgroup's part of the protected list up while the others work.
+template <u32 TY, int W, int MT>
+__global__ __launch_bounds__(1024) void k_few_rows(Few f)
+{
+    typedef typename Elem<TY>::type T;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ u64 range[2];
+    __shared__ u32 starts[18];
+    __shared__ __attribute__((aligned(16))) float sums[16 * MT][16], listed[16 * MT][16];
+    u32 *table = (u32 *)lds;
+    f4 *part = (f4 *)(lds + Table<TY, W>::BYTES);
+    const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, waves = (blockDim.x >> 6) - 1u;
+    const u32 n0 = blockIdx.x / f.row_blocks * 16u, m0 = blockIdx.x % f.row_blocks * (16u * MT), K = f.n_in;
+    // the furthest word that a lane may ask for: row n0 + 15, its k rounded up to whole steps
+    const bool safe = (((u64)min(n0 + 15u, f.n_out - 1u) * K + K + 128u) * W >> 5) + W + 2u <= f.w.n_words;
+    const u32 every = waves * 128u;
+    u32 raw[AHEAD][W + 1];
+    if (wave < waves) safe ? few_first<W, true>(f, n0, wave * 128u, every, raw) : few_first<W, false>(f, n0, wave * 128u, every, raw);
+    float s = 1.0f, inv = 1.0f;
+    if (TY == TY_F16) centre_scale(f.w, s, inv);
+    fill_table<TY, W>(f.w, table, s);
+    __syncthreads();
+    if (wave == waves) {
+        const u32 half = lane >> 5;
+        const u64 first = (u64)min(n0 + half * 16u, f.n_out) * K;
+        const u64 at = f.w.n_outlier ? first_listed(f.w, first, lane & 31u, half) : 0;
+        if ((lane & 31u) == 0u) range[half] = at;
+    } else {
+        f4 acc[MT] = {};
+        if (safe)
+            few_steps<TY, W, MT, true>(f, (const char *)table, n0, m0, wave * 128u, every, raw, acc);
+        else
+            few_steps<TY, W, MT, false>(f, (const char *)table, n0, m0, wave * 128u, every, raw, acc);
 #pragma unroll
         for (int t = 0; t < MT; t++) part[(wave * MT + t) * 64u + lane] = acc[t];
     }
     __syncthreads();
+    const u64 lo = range[0], hi = range[1];
+    const u32 rows = min(f.rows - m0, 16u * MT);
+    if (hi > lo) row_starts(f.w, lo, hi, n0, 16u, starts);
     // lane (i, g) of a part holds row i, outputs 4 g .. 4 g + 3
-    float *sums = (float *)(lds + f.sums_at);
     for (u32 j = threadIdx.x; j < MT * 64u; j += blockDim.x) {
         f4 v = part[j];
         for (u32 q = 1; q < waves; q++) v += part[q * MT * 64u + j];
-        *(f4 *)(sums + (j >> 6) * 256u + (j & 15u) * 16u + (j >> 4 & 3u) * 4u) = v;
+        *(f4 *)&sums[(j >> 6) * 16u + (j & 15u)][(j >> 4 & 3u) * 4u] = v;
     }
     __syncthreads();
-    finish<TY, MT>(f, lds, range[0], range[1], m0, n0, inv);
+    if (hi > lo) { // a wave per output
+        for (u32 t = wave; t < 16u; t += waves + 1u) {
+            const u32 count = (u32)(hi - lo), from = min(starts[t], count), to = min(starts[t + 1u], count), base = (n0 + t) * K;
+            if (f.turned) { // four lanes an entry, eight rows each
+                const GLOBAL_AS T *x = (const GLOBAL_AS T *)f.turned + (u64)(m0 / TURNED) * K * TURNED + m0 % TURNED + (lane & 3u) * 8u;
+                float sum[8] = {};
+                for (u32 j = from + (lane >> 2); j < to; j += 16u) {
+                    const u32 k = gptr(f.w.out_idx)[lo + j] - base;
+                    if (k >= K) continue;
+                    const float v = protected_value(f.w, lo + j);
+                    const Raw8<TY> a = load_raw8<TY>(x + (u64)k * TURNED, (lane & 3u) * 8u < 16u * MT ? 8u : 0u);
+#pragma unroll
+                    for (int q = 0; q < 8; q++) sum[q] += v * a[q];
+                }
+#pragma unroll
+                for (int d = 4; d < 64; d <<= 1)
+#pragma unroll
+                    for (int q = 0; q < 8; q++) sum[q] += __shfl_xor(sum[q], d);
+                if (lane < 2u * MT) {
+#pragma unroll
+                    for (int q = 0; q < 8; q++) listed[lane * 8u + q][t] = sum[q];
+                }
+            } else {
+                for (u32 m = 0; m < rows; m++) {
+                    const GLOBAL_AS T *x = (const GLOBAL_AS T *)f.x.p + (u64)(m0 + m) * f.x.stride;
+                    float sum = 0.0f;
+                    for (u32 j = from + lane; j < to; j += 64u) {
+                        const u32 k = gptr(f.w.out_idx)[lo + j] - base;
+                        if (k < K) sum += protected_value(f.w, lo + j) * Elem<TY>::get(x[k]);
+                    }
+#pragma unroll
+                    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+                    if (lane == 0u) listed[m][t] = sum;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    for (u32 j = threadIdx.x; j < rows * 2u; j += blockDim.x) {
+        const u32 m = j >> 1, n = (j & 1u) * 8u;
+        if (n0 + n >= f.n_out) continue;
+        float v[8];
+#pragma unroll
+        for (u32 t = 0; t < 8u; t++) v[t] = sums[m][n + t] * inv + (hi > lo ? listed[m][n + t] : 0.0f);
+        finish8<TY>(f.end, m0 + m, n0 + n, v);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
 // weight [n_in][n_out]
 // ------------------------------------------------------------------------------------------
-// 16 R outputs, 16 MT rows; lane (i, g) decodes outputs i R .. i R + R - 1 of the k's 8 g .. 8 g + 7 of 32.
-template <u32 TY, int W, int MT, int R>
-__global__ __launch_bounds__(1024) void k_few_cols(Few f)
+constexpr u32 SPLIT_COLS = 2048; // outputs of a workgroup: 256 threads, eight each
+constexpr u32 SPLIT_DEPTH = 64;  // most rows of the weight that it walks down
+
+// Rows blockIdx.x % splits * depth .. of the weight.  Table: the values themselves.
+template <u32 TY, int W, int M>
+__global__ __launch_bounds__(256) void k_few_split(Few f)
 {
     typedef typename Elem<TY>::type T;
-    constexpr int ND = (R * W + 31) / 32; // words of a run
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    u32 *table = (u32 *)lds;
-    f4 *part = (f4 *)(lds + Table<TY, W>::BYTES);
-    const u32 wave = threadIdx.x >> 6, lane = threadIdx.x & 63u, waves = blockDim.x >> 6;
-    const u32 n0 = blockIdx.x / f.row_blocks * (16u * R), m0 = blockIdx.x % f.row_blocks * (16u * MT);
-    float s = 1.0f, inv = 1.0f;
-    if (TY == TY_F16) centre_scale(f.w, s, inv);
-    fill_table<TY, W>(f.w, table, s);
-    __syncthreads();
-    const u32 i = lane & 15u, g = lane >> 4, K = f.n_in;
-    const u32 mine = lane_copy<TY, W>();
-    const GLOBAL_AS T *x[MT];
+    typedef Table<TY_BF16, W> Tab; // (one word an entry, as there)
+    constexpr int ND = (8 * W + 31) / 32;
+    constexpr u32 ROWS = 4; // rows asked for before one is worked on
+    __shared__ __attribute__((aligned(16))) u32 table[Tab::BYTES / 4];
+    __shared__ float xs[SPLIT_DEPTH][M];
+    __shared__ float extra[M][SPLIT_COLS];
+    __shared__ u32 starts[SPLIT_DEPTH + 2];
+    __shared__ u64 range[2];
+    const u32 split = blockIdx.x % f.splits, n0 = blockIdx.x / f.splits * SPLIT_COLS, ka = split * f.depth, kn = min(f.depth, f.n_in - ka);
+    const u32 run = threadIdx.x * 8u, n = n0 + run;
+    const u64 first_bit = ((u64)ka * f.n_out + n) * W, row_bits = (u64)f.n_out * W;
+    u32 raw[ROWS][ND + 1];
+    auto ask = [&](u32 j, u32 *d) { // row j of the part
+        const u64 bit = first_bit + j * row_bits;
+        load_words<ND + 1, false>(f.w.packed, bit >> 5, n < f.n_out && j < kn ? f.w.n_words : 0, d);
+    };
 #pragma unroll
-    for (int t = 0; t < MT; t++) {
-        x[t] = (const GLOBAL_AS T *)f.x.p + (u64)min(m0 + 16u * t + i, f.rows - 1u) * f.x.stride;
+    for (u32 j = 0; j < ROWS; j++) ask(j, raw[j]);
+    for (u32 i = threadIdx.x; i < kn * M; i += 256u)
+        xs[i / M][i % M] = i % M < f.rows ? Elem<TY>::get(((const GLOBAL_AS T *)f.x.p)[(u64)(i % M) * f.x.stride + ka + i / M]) : 0.0f;
+    for (u32 i = threadIdx.x; i < (1u << W) * Tab::COPIES; i += 256u) table[i] = __float_as_uint(symbol_value(f.w, i / Tab::COPIES));
+    const bool any = f.w.n_outlier != 0;
+    if (any) {
+        for (u32 i = threadIdx.x; i < M * SPLIT_COLS; i += 256u) extra[i / SPLIT_COLS][i % SPLIT_COLS] = 0.0f;
+        if (threadIdx.x >= 192u) {
+            const u32 lane = threadIdx.x & 63u, half = lane >> 5;
+            const u64 at = first_listed(f.w, (u64)(ka + half * kn) * f.n_out, lane & 31u, half);
+            if ((lane & 31u) == 0u) range[half] = at;
+        }
     }
-    f4 acc[MT][R] = {};
-    const u64 row_bits = (u64)f.n_out * W, run_bit = (u64)(n0 + i * R) * W;
-    for (u32 k0 = wave * 32u; k0 < K; k0 += waves * 32u) {
-        const u32 k = k0 + 8u * g, left = k < K ? K - k : 0u;
-        u32 e[8][R][2];
+    __syncthreads();
+    const u64 lo = any ? range[0] : 0, hi = any ? range[1] : 0;
+    if (hi > lo) row_starts(f.w, lo, hi, ka, kn, starts);
+    const u32 mine = lane_copy<TY_BF16, W>();
+    float acc[M][8] = {};
+    for (u32 j0 = 0; j0 < kn; j0 += ROWS) {
 #pragma unroll
-        for (u32 j = 0; j < 8u; j++) {
-            u32 raw[ND + 1], d[ND + 1];
-            const u64 bit = (u64)(k + j) * row_bits + run_bit;
-            load_words<ND + 1>(f.w.packed, bit >> 5, j < left ? f.w.n_words : 0, raw);
+        for (u32 q = 0; q < ROWS; q++) {
+            const u32 j = j0 + q;
+            if (j >= kn) break;
+            const u32 shift = (u32)(first_bit + j * row_bits) & 31u;
+            u32 d[ND + 1];
 #pragma unroll
-            for (int q = 0; q < ND; q++) d[q] = __builtin_amdgcn_alignbit(raw[q + 1], raw[q], (u32)bit & 31u);
+            for (int t = 0; t < ND; t++) d[t] = __builtin_amdgcn_alignbit(raw[q][t + 1], raw[q][t], shift);
             d[ND] = 0u;
+            ask(j + ROWS, raw[q]);
+            float x[M];
 #pragma unroll
-            for (int t = 0; t < R; t++) look_up<TY, W>((const char *)table, mine, d, t, e[j][t]);
-        }
-        Xs<TY> v[MT];
+            for (int m = 0; m < M; m++) x[m] = xs[j][m];
 #pragma unroll
-        for (int t = 0; t < MT; t++) load_xs<TY>(x[t] + k, left, v[t]);
+            for (int t = 0; t < 8; t++) {
+                u32 e[2];
+                look_up<TY_BF16, W>((const char *)table, mine, d, t, e);
 #pragma unroll
-        for (int q = 0; q < R; q++) {
-            Parts<TY> w;
-#pragma unroll
-            for (int j = 0; j < 4; j++) put_entries<TY>(w, j, e[2 * j][q], e[2 * j + 1][q]);
-#pragma unroll
-            for (int t = 0; t < MT; t++) acc[t][q] = multiply<TY>(w, v[t], acc[t][q]);
-        }
-    }
-    // lane (i, g) of instruction q holds row i, outputs (4 g + c) R + q
-    float *sums = (float *)(lds + f.sums_at);
-#pragma unroll
-    for (int q = 0; q < R; q++) {
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < MT; t++) part[(wave * MT + t) * 64u + lane] = acc[t][q];
-        __syncthreads();
-        for (u32 j = threadIdx.x; j < MT * 64u; j += blockDim.x) {
-            f4 v = part[j];
-            for (u32 o = 1; o < waves; o++) v += part[o * MT * 64u + j];
-#pragma unroll
-            for (u32 c = 0; c < 4u; c++) sums[((j >> 6) * 16u + (j & 15u)) * (16u * R) + ((j >> 4 & 3u) * 4u + c) * R + q] = v[c];
+                for (int m = 0; m < M; m++) acc[m][t] = fmaf(x[m], __uint_as_float(e[0]), acc[m][t]);
+            }
         }
     }
     __syncthreads();
-    finish<TY, MT>(f, lds, 0, f.w.n_outlier, m0, n0, inv);
+    // the protected values row by row: a row has an output once
+    if (hi > lo) {
+        for (u32 j = 0; j < kn; j++) {
+            const u32 count = (u32)(hi - lo), to = min(starts[j + 1u], count);
+            for (u32 q = min(starts[j], count) + threadIdx.x; q < to; q += 256u) {
+                const u32 c = gptr(f.w.out_idx)[lo + q] - (ka + j) * f.n_out - n0;
+                if (c >= SPLIT_COLS || c + n0 >= f.n_out) continue;
+                const float v = protected_value(f.w, lo + q);
+#pragma unroll
+                for (int m = 0; m < M; m++) extra[m][c] = fmaf(xs[j][m], v, extra[m][c]);
+            }
+            __syncthreads();
+        }
+    }
+    if (n >= f.n_out) return;
+#pragma unroll
+    for (int m = 0; m < M; m++) {
+        if ((u32)m >= f.rows) break;
+        f4 a, b;
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            a[t] = acc[m][t] + (any ? extra[m][run + t] : 0.0f);
+            b[t] = acc[m][t + 4] + (any ? extra[m][run + t + 4] : 0.0f);
+        }
+        float *to = f.partial + ((u64)split * f.rows + m) * f.n8 + n;
+        *(f4 *)to = a;
+        *(f4 *)(to + 4) = b;
+    }
+}
+
+// 64 outputs of a row: thread (part, i) adds the splits part, part + 32, ... of outputs 8 i .. 8 i + 7.
+template <u32 TY>
+__global__ __launch_bounds__(256) void k_few_join(Few f)
+{
+    __shared__ __attribute__((aligned(16))) float sums[32][64];
+    const u32 blocks = (f.n_out + 63u) / 64u, m = blockIdx.x / blocks, n0 = blockIdx.x % blocks * 64u;
+    const u32 i = (threadIdx.x & 7u) * 8u, part = threadIdx.x >> 3;
+    f4 a = {}, b = {};
+    if (n0 + i < f.n_out) {
+#pragma unroll 8
+        for (u32 q = part; q < f.splits; q += 32u) {
+            const GLOBAL_AS f4 *p = (const GLOBAL_AS f4 *)(gptr(f.partial) + ((u64)q * f.rows + m) * f.n8 + n0 + i);
+            a += p[0];
+            b += p[1];
+        }
+    }
+    *(f4 *)&sums[part][i] = a;
+    *(f4 *)&sums[part][i + 4] = b;
+    for (u32 d = 16; d; d >>= 1) {
+        __syncthreads();
+        if (part < d) {
+            *(f4 *)&sums[part][i] += *(const f4 *)&sums[part + d][i];
+            *(f4 *)&sums[part][i + 4] += *(const f4 *)&sums[part + d][i + 4];
+        }
+    }
+    if (part == 0u && n0 + i < f.n_out) {
+        float v[8];
+#pragma unroll
+        for (u32 t = 0; t < 8u; t++) v[t] = sums[0][i + t];
+        finish8<TY>(f.end, m, n0 + i, v);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -351,52 +469,79 @@ __global__ __launch_bounds__(1024) void k_few_cols(Few f)
 // ------------------------------------------------------------------------------------------
 namespace {
 
+struct FewRoom {
+    u64 turned = 0, partial = 0; // bytes of either (never both)
+    u32 splits = 1, depth = 1;
+    FewRoom(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed)
+    {
+        if (!in_out) {
+            if (listed && rows > FEW_TURNED) turned = (rows + TURNED - 1) / TURNED * TURNED * n_in * elem_size(type);
+            return;
+        }
+        // about 768 workgroups (three a CU) where the weight has 4 rows for each at least, SPLIT_DEPTH at most
+        const u32 blocks = (n_out + SPLIT_COLS - 1u) / SPLIT_COLS;
+        depth = (u32)(((u64)n_in * blocks + 767u) / 768u);
+        depth = depth < 4u ? 4u : depth > SPLIT_DEPTH ? SPLIT_DEPTH : depth;
+        splits = (n_in + depth - 1u) / depth;
+        partial = (u64)splits * rows * ((n_out + 7u) / 8u * 8u) * 4u;
+    }
+};
+
 template <u32 TY, int W, int MT>
 void start_rows(Few &f, hipStream_t s)
 {
     // waves: enough for four to a SIMD over all workgroups, each with two steps of 128 at least where there are as many
     const u32 groups = (f.n_out + 15u) / 16u * f.row_blocks, steps = (f.n_in + 127u) / 128u;
     u32 waves = 4;
-    while (waves < 15u && waves * groups < 4096u && waves * 2u < steps) waves = min(waves * 2u, 15u);
-    f.cols = 16;
-    f.sums_at = Table<TY, W>::BYTES + waves * MT * 1024u;
-    f.listed_at = f.sums_at + MT * 1024u;
-    const u32 lds = f.listed_at + (f.w.n_outlier ? MT * 2048u : 0u);
-    PROF("k_few_rows", s, k_few_rows<TY, W, MT><<<groups, 64u * (waves + 1u), lds, s>>>(f));
-}
-template <u32 TY, int W, int MT, int R>
-void start_cols_of(Few &f, hipStream_t s)
-{
-    const u32 groups = (f.n_out + 16u * R - 1u) / (16u * R) * f.row_blocks, steps = (f.n_in + 31u) / 32u;
-    u32 waves = 4;
-    while (waves < 16u / MT && waves * groups < 4096u && waves * 2u < steps) waves *= 2u; // (64 KB of LDS at most)
-    f.cols = 16u * R;
-    f.sums_at = Table<TY, W>::BYTES + waves * MT * 1024u;
-    f.listed_at = f.sums_at + MT * R * 1024u;
-    const u32 lds = f.listed_at + (f.w.n_outlier ? MT * R * 2048u : 0u);
-    PROF("k_few_cols", s, k_few_cols<TY, W, MT, R><<<groups, 64u * waves, lds, s>>>(f));
-}
-template <u32 TY, int W, int MT>
-void start(Few &f, hipStream_t s)
-{
-    if (!f.in_out)
-        start_rows<TY, W, MT>(f, s);
-    else
-        start_cols_of<TY, W, MT, TY == TY_F32 ? 2 : 4>(f, s);
+    while (waves < 15u && waves * groups < 4096u && waves * 2u < steps) waves = waves * 2u < 15u ? waves * 2u : 15u;
+    PROF("k_few_rows", s, k_few_rows<TY, W, MT><<<groups, 64u * (waves + 1u), Table<TY, W>::BYTES + waves * MT * 1024u, s>>>(f));
 }
 template <u32 TY>
-void start_mt(Few &f, hipStream_t s)
+void start_turn(const LinearCall &c, hipStream_t s)
 {
-    if (f.rows <= 16u) {
-        f.row_blocks = 1;
-        with_width(f.w.w, [&](auto w) { start<TY, decltype(w)::value, 1>(f, s); });
-    } else {
-        f.row_blocks = (f.rows + 31u) / 32u;
-        with_width(f.w.w, [&](auto w) { start<TY, decltype(w)::value, 2>(f, s); });
+    PROF("k_few_turn", s, k_few_turn<TY><<<dim3((c.n_in + 63u) / 64u, ((u32)c.rows + TURNED - 1u) / TURNED), 256, 0, s>>>(
+                              c.x, (u32)c.rows, c.n_in, (typename Elem<TY>::type *)c.ws));
+}
+template <u32 TY>
+void start_few(Few &f, const LinearCall &c, hipStream_t s)
+{
+    const FewRoom r(c.rows, c.n_in, c.n_out, c.in_out != 0, c.type, c.w.n_outlier != 0);
+    if (!c.in_out) {
+        if (r.turned) {
+            start_turn<TY>(c, s);
+            f.turned = c.ws;
+        }
+        f.row_blocks = f.rows <= 16u ? 1u : (f.rows + 31u) / 32u;
+        with_width(f.w.w, [&](auto w) {
+            if (f.rows <= 16u)
+                start_rows<TY, decltype(w)::value, 1>(f, s);
+            else
+                start_rows<TY, decltype(w)::value, 2>(f, s);
+        });
+        return;
     }
+    f.partial = (float *)c.ws;
+    f.splits = r.splits;
+    f.depth = r.depth;
+    f.n8 = (f.n_out + 7u) / 8u * 8u;
+    const u32 grid = r.splits * ((f.n_out + SPLIT_COLS - 1u) / SPLIT_COLS);
+    with_width(f.w.w, [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        if (f.rows == 1u)
+            PROF("k_few_split", s, k_few_split<TY, W, 1><<<grid, 256, 0, s>>>(f));
+        else
+            PROF("k_few_split", s, k_few_split<TY, W, (int)FEW_SPLIT><<<grid, 256, 0, s>>>(f));
+    });
+    PROF("k_few_join", s, k_few_join<TY><<<f.rows * ((f.n_out + 63u) / 64u), 256, 0, s>>>(f));
 }
 
 } // namespace
+
+u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed)
+{
+    const FewRoom r(rows, n_in, n_out, in_out, type, listed);
+    return rows ? r.turned + r.partial : 0;
+}
 
 hipError_t launch_few(const LinearCall &c, hipStream_t s)
 {
@@ -407,11 +552,10 @@ hipError_t launch_few(const LinearCall &c, hipStream_t s)
     f.rows = (u32)c.rows;
     f.n_in = c.n_in;
     f.n_out = c.n_out;
-    f.in_out = c.in_out;
     switch (c.type) {
-    case TY_F32: start_mt<TY_F32>(f, s); break;
-    case TY_BF16: start_mt<TY_BF16>(f, s); break;
-    default: start_mt<TY_F16>(f, s); break;
+    case TY_F32: start_few<TY_F32>(f, c, s); break;
+    case TY_BF16: start_few<TY_BF16>(f, c, s); break;
+    default: start_few<TY_F16>(f, c, s); break;
     }
     return hipGetLastError();
 }

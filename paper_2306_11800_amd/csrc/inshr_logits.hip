@@ -479,7 +479,7 @@ namespace {
 
 // A workgroup per row: 256 threads where the rows fill the chip (eight workgroups a CU), 1024 where there are few, each of
 // which is then read in fewer steps.
-constexpr u64 FEW_ROWS = 512;
+constexpr u64 FEW_LOGIT_ROWS = 512;
 
 template <u32 TY, u32 BLOCK>
 void start_top(const LogitsCall &c, int *index, float *value, float *tail, hipStream_t s)
@@ -502,7 +502,7 @@ void start_grad(const LogitsCall &c, const double *saved, const float *g, const 
 hipError_t launch_top_logits(const LogitsCall &c, int *index, float *value, float *tail, hipStream_t s)
 {
     // (k of 1024 threads' maxima: every wave has to have seen k / 16 elements' worth of them)
-    const bool few = c.rows < FEW_ROWS && c.n_vocab >= 8192u;
+    const bool few = c.rows < FEW_LOGIT_ROWS && c.n_vocab >= 8192u;
     switch (c.type) {
     case TY_F32: few ? start_top<TY_F32, 1024>(c, index, value, tail, s) : start_top<TY_F32, 256>(c, index, value, tail, s); break;
     case TY_BF16: few ? start_top<TY_BF16, 1024>(c, index, value, tail, s) : start_top<TY_BF16, 256>(c, index, value, tail, s); break;
@@ -512,7 +512,7 @@ hipError_t launch_top_logits(const LogitsCall &c, int *index, float *value, floa
 }
 hipError_t launch_distill(const LogitsCall &c, float *loss, double *saved, hipStream_t s)
 {
-    const bool few = c.rows < FEW_ROWS;
+    const bool few = c.rows < FEW_LOGIT_ROWS;
     switch (c.type) {
     case TY_F32: few ? start_distill<TY_F32, 1024>(c, loss, saved, s) : start_distill<TY_F32, 256>(c, loss, saved, s); break;
     case TY_BF16: few ? start_distill<TY_BF16, 1024>(c, loss, saved, s) : start_distill<TY_BF16, 256>(c, loss, saved, s); break;
@@ -522,7 +522,7 @@ hipError_t launch_distill(const LogitsCall &c, float *loss, double *saved, hipSt
 }
 hipError_t launch_distill_grad(const LogitsCall &c, const double *saved, const float *g, const Mat &grad, hipStream_t s)
 {
-    const bool few = c.rows < FEW_ROWS;
+    const bool few = c.rows < FEW_LOGIT_ROWS;
     switch (c.type) {
     case TY_F32: few ? start_grad<TY_F32, 1024>(c, saved, g, grad, s) : start_grad<TY_F32, 256>(c, saved, g, grad, s); break;
     case TY_BF16: few ? start_grad<TY_BF16, 1024>(c, saved, g, grad, s) : start_grad<TY_BF16, 256>(c, saved, g, grad, s); break;

@@ -92,12 +92,12 @@ __device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdg
 // the stream
 // ------------------------------------------------------------------------------------------
 typedef u32 u4_any __attribute__((ext_vector_type(4), aligned(4)));
-// N consecutive words, those from word `end` on as 0.
-template <int N>
+// N consecutive words, those from word `end` on as 0.  SAFE: they are there whatever `end` says.
+template <int N, bool SAFE = false>
 __device__ __forceinline__ void load_words(const u32 *packed, u64 at, u64 end, u32 *d)
 {
     const GLOBAL_AS u32 *p = gptr(packed) + at;
-    if (at + N <= end) {
+    if (SAFE || at + N <= end) {
 #pragma unroll
         for (int i = 0; i + 4 <= N; i += 4) {
             const u4_any v = *(const GLOBAL_AS u4_any *)(p + i);
