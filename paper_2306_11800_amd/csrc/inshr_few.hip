@@ -138,26 +138,42 @@ __device__ __forceinline__ void row_starts(const WDesc &w, u64 lo, u64 hi, u32 r
 // weight [n_out][n_in]
 // ------------------------------------------------------------------------------------------
 constexpr u32 TURNED = 32; // rows of activations side by side in their turned copy
-constexpr u32 FEW_TURNED = 4; // up to as many rows the protected values' activations are taken from the rows themselves
+constexpr u32 FEW_PLAIN = 4; // up to as many rows are read as they are
 
 struct Few {
     WDesc w;
     Finish end;
     Mat x;
-    const void *turned; // [row blocks of TURNED][n_in][TURNED] activations, or NULL
+    const Frag *packed; // k_few_pack's, or NULL
+    const void *turned;
+    u32 steps;          // of 128 of the reduction
     float *partial;     // k_few_split: [splits][rows][n8]
     u32 rows, n_in, n_out, n8;
     u32 row_blocks;     // blocks of 16 MT rows
     u32 splits, depth;  // k_few_split: parts of the reduction, rows of a part
 };
 
-// x turned: blocks of TURNED rows, so that the activations that a protected value meets lie side by side.
+// What the other kernels read of more than FEW_PLAIN rows of x, so that their loads take whole lines (16 rows of x a load
+// were 64 pieces of 16 bytes, and the 512 cycles that a CU takes for a step's addresses were all of its time):
+//   packed  the operands of the matrix cores, [tile of 16 rows][step of 128][4 instructions][parts][64 lanes][8]
+//   turned  blocks of TURNED rows, the activations that a protected value meets side by side
+// The first `tiles * steps` workgroups pack, the others turn.
 template <u32 TY>
-__global__ __launch_bounds__(256) void k_few_turn(Mat x, u32 rows, u32 cols, typename Elem<TY>::type *__restrict__ to)
+__global__ __launch_bounds__(256) void k_few_pack(Mat x, u32 rows, u32 cols, u32 tiles, u32 steps, Frag *__restrict__ packed,
+                                                  typename Elem<TY>::type *__restrict__ turned)
 {
     typedef typename Elem<TY>::type T;
+    if (blockIdx.x < tiles * steps) {
+        const u32 tile = blockIdx.x / steps, kb = blockIdx.x % steps, s = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+        const u32 r = tile * 16u + (lane & 15u), k = kb * 128u + 32u * (lane >> 4) + 8u * s;
+        Xs<TY> v;
+        load_xs<TY>((const GLOBAL_AS T *)x.p + (u64)min(r, rows - 1u) * x.stride + k, k < cols && r < rows ? cols - k : 0u, v);
+#pragma unroll
+        for (int q = 0; q < Xs<TY>::N; q++) packed[((u64)(blockIdx.x * 4u + s) * Xs<TY>::N + q) * 64u + lane] = v.p[q];
+        return;
+    }
     __shared__ T tile[64][TURNED + 2];
-    const u32 c0 = blockIdx.x * 64u, r0 = blockIdx.y * TURNED;
+    const u32 id = blockIdx.x - tiles * steps, across = (cols + 63u) / 64u, c0 = id % across * 64u, block = id / across, r0 = block * TURNED;
     for (u32 i = threadIdx.x; i < 64u * TURNED; i += 256u) {
         const u32 r = r0 + i / 64u, c = c0 + i % 64u;
         tile[i % 64u][i / 64u] = r < rows && c < cols ? ((const GLOBAL_AS T *)x.p)[(u64)r * x.stride + c] : (T)0;
@@ -165,14 +181,14 @@ __global__ __launch_bounds__(256) void k_few_turn(Mat x, u32 rows, u32 cols, typ
     __syncthreads();
     for (u32 i = threadIdx.x; i < 64u * TURNED; i += 256u) {
         const u32 c = i / TURNED;
-        if (c0 + c < cols) to[((u64)blockIdx.y * cols + c0 + c) * TURNED + i % TURNED] = tile[c][i % TURNED];
+        if (c0 + c < cols) turned[((u64)block * cols + c0 + c) * TURNED + i % TURNED] = tile[c][i % TURNED];
     }
 }
 
 constexpr u32 AHEAD = 2; // steps whose part of the stream is asked for before one is worked on
 
 // This wave's steps of 128 of the reduction, `every` apart.  SAFE: no load of the stream can lead past its end.
-template <u32 TY, int W, int MT, bool SAFE>
+template <u32 TY, int W, int MT, bool PACKED, bool SAFE>
 __device__ __forceinline__ void few_steps(const Few &f, const char *table, u32 n0, u32 m0, u32 k0, u32 every, u32 (&raw)[AHEAD][W + 1], f4 (&acc)[MT])
 {
     typedef typename Elem<TY>::type T;
@@ -181,7 +197,7 @@ __device__ __forceinline__ void few_steps(const Few &f, const char *table, u32 n
     const u32 mine = lane_copy<TY, W>();
     const GLOBAL_AS T *x[MT];
 #pragma unroll
-    for (int t = 0; t < MT; t++) x[t] = (const GLOBAL_AS T *)f.x.p + (u64)min(m0 + 16u * t + i, f.rows - 1u) * f.x.stride;
+    for (int t = 0; t < MT; t++) x[t] = PACKED ? nullptr : (const GLOBAL_AS T *)f.x.p + (u64)min(m0 + 16u * t + i, f.rows - 1u) * f.x.stride;
     for (; k0 < K; k0 += AHEAD * every) {
 #pragma unroll
         for (u32 ahead = 0; ahead < AHEAD; ahead++) {
@@ -215,7 +231,13 @@ __device__ __forceinline__ void few_steps(const Few &f, const char *table, u32 n
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
                     Xs<TY> v;
-                    load_xs<TY>(x[t] + k + 8u * s, full ? 8u : left > 8u * s ? left - 8u * s : 0u, v);
+                    if (PACKED) {
+                        const Frag *p = f.packed + ((u64)((m0 / 16u + t) * f.steps + kb / 128u) * 4u + s) * (Xs<TY>::N * 64u) + lane;
+#pragma unroll
+                        for (int q = 0; q < Xs<TY>::N; q++) v.p[q].q = *(const GLOBAL_AS u4_16 *)&gptr(p)[q * 64].q;
+                    } else {
+                        load_xs<TY>(x[t] + k + 8u * s, full ? 8u : left > 8u * s ? left - 8u * s : 0u, v);
+                    }
                     acc[t] = multiply<TY>(w, v, acc[t]);
                 }
             }
@@ -236,8 +258,38 @@ __device__ __forceinline__ void few_first(const Few &f, u32 n0, u32 k0, u32 ever
     }
 }
 
+// Up to FEW_PLAIN rows: the protected values' part of 16 outputs, by one wave while the others work on the stream.  64 entries
+// at a time; the entries of an output follow each other and are added up by a scan, and the last one's lane has the sum.
+template <u32 TY>
+__device__ __forceinline__ void listed_by_wave(const Few &f, u64 lo, u64 hi, u32 n0, float (*listed)[16])
+{
+    typedef typename Elem<TY>::type T;
+    const u32 lane = threadIdx.x & 63u, K = f.n_in;
+    if (lane < 16u)
+        for (u32 m = 0; m < f.rows; m++) listed[m][lane] = 0.0f;
+    for (u64 j0 = lo; j0 < hi; j0 += 64u) {
+        const u64 j = j0 + lane;
+        const u32 at = j < hi ? gptr(f.w.out_idx)[j] : 0u, row = at / K, k = at - row * K;
+        const bool mine = j < hi && row - n0 < 16u;
+        const u32 t = mine ? row - n0 : 16u + lane; // (the others: outputs of their own)
+        const float v = mine ? protected_value(f.w, j) : 0.0f;
+        const u32 after = __shfl_down(t, 1);
+        const bool last = mine && (lane == 63u || after != t);
+        for (u32 m = 0; m < f.rows; m++) {
+            float p = mine ? v * Elem<TY>::get(((const GLOBAL_AS T *)f.x.p)[(u64)m * f.x.stride + k]) : 0.0f;
+#pragma unroll
+            for (u32 d = 1; d < 64u; d <<= 1) {
+                const float up = __shfl_up(p, d);
+                const u32 whose = __shfl_up(t, d);
+                if (lane >= d && whose == t) p += up;
+            }
+            if (last) listed[m][t] += p;
+        }
+    }
+}
+
 // 16 outputs, 16 MT rows; the last wave looks the workgroup's part of the protected list up while the others work.
-template <u32 TY, int W, int MT>
+template <u32 TY, int W, int MT, bool PACKED>
 __global__ __launch_bounds__(1024) void k_few_rows(Few f)
 {
     typedef typename Elem<TY>::type T;
@@ -263,19 +315,20 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
         const u64 first = (u64)min(n0 + half * 16u, f.n_out) * K;
         const u64 at = f.w.n_outlier ? first_listed(f.w, first, lane & 31u, half) : 0;
         if ((lane & 31u) == 0u) range[half] = at;
+        if (!PACKED) listed_by_wave<TY>(f, __shfl(at, 0), __shfl(at, 32), n0, listed);
     } else {
         f4 acc[MT] = {};
         if (safe)
-            few_steps<TY, W, MT, true>(f, (const char *)table, n0, m0, wave * 128u, every, raw, acc);
+            few_steps<TY, W, MT, PACKED, true>(f, (const char *)table, n0, m0, wave * 128u, every, raw, acc);
         else
-            few_steps<TY, W, MT, false>(f, (const char *)table, n0, m0, wave * 128u, every, raw, acc);
+            few_steps<TY, W, MT, PACKED, false>(f, (const char *)table, n0, m0, wave * 128u, every, raw, acc);
 #pragma unroll
         for (int t = 0; t < MT; t++) part[(wave * MT + t) * 64u + lane] = acc[t];
     }
     __syncthreads();
     const u64 lo = range[0], hi = range[1];
     const u32 rows = min(f.rows - m0, 16u * MT);
-    if (hi > lo) row_starts(f.w, lo, hi, n0, 16u, starts);
+    if (PACKED && hi > lo) row_starts(f.w, lo, hi, n0, 16u, starts);
     // lane (i, g) of a part holds row i, outputs 4 g .. 4 g + 3
     for (u32 j = threadIdx.x; j < MT * 64u; j += blockDim.x) {
         f4 v = part[j];
@@ -283,40 +336,36 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
         *(f4 *)&sums[(j >> 6) * 16u + (j & 15u)][(j >> 4 & 3u) * 4u] = v;
     }
     __syncthreads();
-    if (hi > lo) { // a wave per output
+    if (PACKED && hi > lo) { // a wave per output; four lanes an entry, eight rows each, four entries a lane at a time
         for (u32 t = wave; t < 16u; t += waves + 1u) {
             const u32 count = (u32)(hi - lo), from = min(starts[t], count), to = min(starts[t + 1u], count), base = (n0 + t) * K;
-            if (f.turned) { // four lanes an entry, eight rows each
-                const GLOBAL_AS T *x = (const GLOBAL_AS T *)f.turned + (u64)(m0 / TURNED) * K * TURNED + m0 % TURNED + (lane & 3u) * 8u;
-                float sum[8] = {};
-                for (u32 j = from + (lane >> 2); j < to; j += 16u) {
-                    const u32 k = gptr(f.w.out_idx)[lo + j] - base;
-                    if (k >= K) continue;
-                    const float v = protected_value(f.w, lo + j);
-                    const Raw8<TY> a = load_raw8<TY>(x + (u64)k * TURNED, (lane & 3u) * 8u < 16u * MT ? 8u : 0u);
+            const GLOBAL_AS T *x = (const GLOBAL_AS T *)f.turned + (u64)(m0 / TURNED) * K * TURNED + (lane & 3u) * 8u;
+            float sum[8] = {};
+            for (u32 j0 = from + (lane >> 2); j0 < to; j0 += 64u) {
+                u32 k[4];
+                float v[4];
+                Raw8<TY> a[4];
 #pragma unroll
-                    for (int q = 0; q < 8; q++) sum[q] += v * a[q];
+                for (u32 q = 0; q < 4u; q++) {
+                    const u32 j = min(j0 + 16u * q, to - 1u);
+                    k[q] = gptr(f.w.out_idx)[lo + j] - base;
+                    v[q] = j0 + 16u * q < to && k[q] < K ? protected_value(f.w, lo + j) : 0.0f;
+                    k[q] = min(k[q], K - 1u);
                 }
 #pragma unroll
-                for (int d = 4; d < 64; d <<= 1)
+                for (u32 q = 0; q < 4u; q++) a[q] = load_raw8<TY>(x + (u64)k[q] * TURNED, 8u);
 #pragma unroll
-                    for (int q = 0; q < 8; q++) sum[q] += __shfl_xor(sum[q], d);
-                if (lane < 2u * MT) {
+                for (u32 q = 0; q < 4u; q++)
 #pragma unroll
-                    for (int q = 0; q < 8; q++) listed[lane * 8u + q][t] = sum[q];
-                }
-            } else {
-                for (u32 m = 0; m < rows; m++) {
-                    const GLOBAL_AS T *x = (const GLOBAL_AS T *)f.x.p + (u64)(m0 + m) * f.x.stride;
-                    float sum = 0.0f;
-                    for (u32 j = from + lane; j < to; j += 64u) {
-                        const u32 k = gptr(f.w.out_idx)[lo + j] - base;
-                        if (k < K) sum += protected_value(f.w, lo + j) * Elem<TY>::get(x[k]);
-                    }
+                    for (int i = 0; i < 8; i++) sum[i] += v[q] != 0.0f ? v[q] * a[q][i] : 0.0f;
+            }
 #pragma unroll
-                    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-                    if (lane == 0u) listed[m][t] = sum;
-                }
+            for (int d = 4; d < 64; d <<= 1)
+#pragma unroll
+                for (int q = 0; q < 8; q++) sum[q] += __shfl_xor(sum[q], d);
+            if (lane < 2u * MT) {
+#pragma unroll
+                for (int q = 0; q < 8; q++) listed[lane * 8u + q][t] = sum[q];
             }
         }
         __syncthreads();
@@ -470,12 +519,17 @@ __global__ __launch_bounds__(256) void k_few_join(Few f)
 namespace {
 
 struct FewRoom {
-    u64 turned = 0, partial = 0; // bytes of either (never both)
+    u64 packed = 0, turned = 0, partial = 0; // bytes (the last, or the others)
+    u32 tiles = 0, steps = 0;                // of `packed`
     u32 splits = 1, depth = 1;
     FewRoom(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed)
     {
         if (!in_out) {
-            if (listed && rows > FEW_TURNED) turned = (rows + TURNED - 1) / TURNED * TURNED * n_in * elem_size(type);
+            steps = (n_in + 127u) / 128u;
+            if (rows <= FEW_PLAIN) return;
+            tiles = rows <= 16u ? 1u : ((u32)rows + 31u) / 32u * 2u;
+            packed = (u64)tiles * steps * 4096u * (type == TY_F32 ? Xs<TY_F32>::N : 1);
+            if (listed) turned = (rows + TURNED - 1) / TURNED * TURNED * n_in * elem_size(type);
             return;
         }
         // about 768 workgroups (three a CU) where the weight has 4 rows for each at least, SPLIT_DEPTH at most
@@ -487,36 +541,38 @@ struct FewRoom {
     }
 };
 
-template <u32 TY, int W, int MT>
+template <u32 TY, int W, int MT, bool PACKED>
 void start_rows(Few &f, hipStream_t s)
 {
-    // waves: enough for four to a SIMD over all workgroups, each with two steps of 128 at least where there are as many
-    const u32 groups = (f.n_out + 15u) / 16u * f.row_blocks, steps = (f.n_in + 127u) / 128u;
-    u32 waves = 4;
-    while (waves < 15u && waves * groups < 4096u && waves * 2u < steps) waves = waves * 2u < 15u ? waves * 2u : 15u;
-    PROF("k_few_rows", s, k_few_rows<TY, W, MT><<<groups, 64u * (waves + 1u), Table<TY, W>::BYTES + waves * MT * 1024u, s>>>(f));
-}
-template <u32 TY>
-void start_turn(const LinearCall &c, hipStream_t s)
-{
-    PROF("k_few_turn", s, k_few_turn<TY><<<dim3((c.n_in + 63u) / 64u, ((u32)c.rows + TURNED - 1u) / TURNED), 256, 0, s>>>(
-                              c.x, (u32)c.rows, c.n_in, (typename Elem<TY>::type *)c.ws));
+    // As many waves as let all workgroups run at once at 16 waves a CU (a round of workgroups that is partly empty costs
+    // more than longer waves: 688 of 9 waves 31 us, of 5 waves 20), but not more than there are steps for.
+    const u32 groups = (f.n_out + 15u) / 16u * f.row_blocks, per_cu = (groups + 255u) / 256u;
+    u32 waves = per_cu >= 5u ? 2u : 16u / per_cu - 1u;
+    waves = waves < f.steps ? waves : f.steps;
+    PROF("k_few_rows", s, k_few_rows<TY, W, MT, PACKED><<<groups, 64u * (waves + 1u), Table<TY, W>::BYTES + waves * MT * 1024u, s>>>(f));
 }
 template <u32 TY>
 void start_few(Few &f, const LinearCall &c, hipStream_t s)
 {
     const FewRoom r(c.rows, c.n_in, c.n_out, c.in_out != 0, c.type, c.w.n_outlier != 0);
     if (!c.in_out) {
-        if (r.turned) {
-            start_turn<TY>(c, s);
-            f.turned = c.ws;
-        }
+        f.steps = r.steps;
         f.row_blocks = f.rows <= 16u ? 1u : (f.rows + 31u) / 32u;
+        if (r.packed) {
+            f.packed = (const Frag *)c.ws;
+            f.turned = c.ws + r.packed;
+            const u32 grid = r.tiles * r.steps + (r.turned ? (c.n_in + 63u) / 64u * ((f.rows + TURNED - 1u) / TURNED) : 0u);
+            PROF("k_few_pack", s, k_few_pack<TY><<<grid, 256, 0, s>>>(c.x, f.rows, c.n_in, r.tiles, r.steps, (Frag *)c.ws,
+                                                                      (typename Elem<TY>::type *)(c.ws + r.packed)));
+        }
         with_width(f.w.w, [&](auto w) {
-            if (f.rows <= 16u)
-                start_rows<TY, decltype(w)::value, 1>(f, s);
+            constexpr int W = decltype(w)::value;
+            if (f.rows <= FEW_PLAIN)
+                start_rows<TY, W, 1, false>(f, s);
+            else if (f.rows <= 16u)
+                start_rows<TY, W, 1, true>(f, s);
             else
-                start_rows<TY, decltype(w)::value, 2>(f, s);
+                start_rows<TY, W, 2, true>(f, s);
         });
         return;
     }
@@ -540,7 +596,7 @@ void start_few(Few &f, const LinearCall &c, hipStream_t s)
 u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed)
 {
     const FewRoom r(rows, n_in, n_out, in_out, type, listed);
-    return rows ? r.turned + r.partial : 0;
+    return rows ? r.packed + r.turned + r.partial : 0;
 }
 
 hipError_t launch_few(const LinearCall &c, hipStream_t s)
