@@ -2,11 +2,15 @@
 host, with and without the regrouping by the previous symbol (Sec. 6; the shape of the paper's delta
 ablation).  Synthetic GPT-2-medium-shaped weights with Adam state, five steps.
 
-    python -m paper_2306_11800_amd.ratio_report [--scale 0.25] [--threads 16] [--bins sketch]
+    python -m paper_2306_11800_amd.ratio_report [--scale 0.25] [--threads 16] [--bins sketch] [--quality 256]
 
 --bins sketch keeps the prune / protect fractions the grid search chose and takes the bins from the
 sketch + weighted K-Means rule with the fewest bits that meet eps (inshr_search_sketch; the same
 uniform numbers at every step).
+
+--quality ROWS also runs that many rows of random hidden states through the layers the model ends with, from the original
+weights and from the compressed ones, and adds to every step the mean divergence of the answers (quality_loss, in nats) and
+the share of rows whose most likely token stays (quality_top1).
 
 Prints one JSON line per step and a summary line.  Bytes of a step = entropy-coded delta streams +
 codebooks + protected values (index and value, 8 bytes each) + group offsets.
@@ -19,7 +23,7 @@ from concurrent.futures import ThreadPoolExecutor
 import numpy as np
 import torch
 
-from . import api, synth
+from . import api, quality, synth
 
 
 def unpack(words: torch.Tensor, n: int, w: int) -> torch.Tensor:
@@ -42,12 +46,15 @@ def main():
     ap.add_argument("--threads", type=int, default=16)
     ap.add_argument("--steps", type=int, default=5)
     ap.add_argument("--bins", choices=["equal", "sketch"], default="equal")
+    ap.add_argument("--quality", type=int, default=0, metavar="ROWS", help="rows of hidden states to compare answers on")
     args = ap.parse_args()
     dev = torch.device("cuda:0")
     ctx = api.Context(dev)
     grid, eps = synth.grid_full(), synth.EPS_DEFAULT
     items = list(synth.gpt2_medium_steps(scale=args.scale, n_steps=args.steps))
     n_total = sum(st[0].size for _, st in items)
+    hidden = synth.gpt2_medium_shapes()[0][1][1]
+    rows = torch.randn((args.quality, hidden), generator=torch.Generator().manual_seed(11)).to(dev)
     q_prev = None
     totals = dict(fp32=0, quantized=0, regrouped=0, index_order=0)
     for t in range(args.steps):
@@ -62,6 +69,10 @@ def main():
         quantized = sum((q.n * q.sym_bits + 7) // 8 for q in q_cur) + side
         line = dict(step=t, fp32_bytes=4 * n_total, quantized_bytes=quantized,
                     mean_symbol_bits=round(sum(q.n * q.sym_bits for q in q_cur) / n_total, 3))
+        if args.quality:
+            steps = quality.gpt2_ending([n for n, _ in items], ts, q_cur, ctx, hidden)
+            kept = quality.degradation(ctx, steps, rows, k=min(64, steps[-1].layer.n_out))
+            line.update(quality_loss=round(kept["loss"], 6), quality_top1=round(kept["top1"], 4))
         if q_prev is not None:
             ds = ctx.delta(q_prev, q_cur, want_perm=True)
             ctx.sync()
