@@ -361,16 +361,17 @@ def _matrix(t: Optional[torch.Tensor], rows, cols, dtype, device, name):
     """The C matrix of a 2-D tensor with elements of a row side by side."""
     if t is None:
         return _NO_MATRIX
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+    stride = t.stride()
+    if t.shape != (rows, cols) or t.dtype != dtype or t.device != device or (cols > 1 and stride[1] != 1):
         raise ValueError(f"{name} must be a {dtype} tensor [{rows}, {cols}] on {device} with rows of adjacent elements")
     # (torch leaves the stride of a single row open, and an output needs one)
-    return CMatrix(t.data_ptr(), t.stride(0) if rows > 1 else cols)
+    return CMatrix(t.data_ptr(), stride[0] if rows > 1 else cols)
 
 
 def _vector(t: Optional[torch.Tensor], shape, dtype, device, name):
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}")
     return t.data_ptr()
 
@@ -478,6 +479,7 @@ class Context:
         idx = self.device.index if self.device.index is not None else 0
         self._device = torch.device(self.device.type, idx)  # (as tensors name it)
         self.stream = torch.cuda.current_stream(self.device)
+        self._stream_ptr = self.stream.cuda_stream
         h = C.c_void_p()
         rc = self.lib.inshr_create(C.byref(h), idx, C.c_void_p(self.stream.cuda_stream), scratch_bytes)
         if rc:
@@ -978,12 +980,13 @@ class Context:
         """Where torch works on another stream than the context's: the context's waits for it and it for the context's
         afterwards, the tensors (and layers) in use are kept from being reused too early, and what is allocated
         meanwhile belongs to the context's stream."""
-        return _Turn(self.stream, used) if torch.cuda.current_stream(self.device) != self.stream else _NO_TURN
+        return _NO_TURN if _current_stream(self._device.index) == self._stream_ptr else _Turn(self.stream, used)
 
     def _rows_of(self, t: torch.Tensor, cols: int, name: str):
-        if t.dim() != 2 or t.shape[1] != cols or t.dtype not in _TYPES or t.device != self._device:
+        shape, type_ = t.shape, _TYPES.get(t.dtype)
+        if len(shape) != 2 or shape[1] != cols or type_ is None or t.device != self._device:
             raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor [rows, {cols}] on {self._device}")
-        return t.shape[0], _TYPES[t.dtype]
+        return shape[0], type_
 
     def linear(self, layer: QuantizedLayer, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
                out: Optional[torch.Tensor] = None, want_pre: bool = False):
@@ -1096,6 +1099,11 @@ class Context:
         with self._enter(logits, top.index, top.value, top.tail, saved, grad_loss, grad):
             self._check(self.lib.inshr_distill_grad(self.h, C.byref(c), cs, cg, co))
         return grad
+
+
+# the current stream's handle (torch.cuda.current_stream makes a Stream object of it, which takes as long as a small kernel)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class _NoTurn:
