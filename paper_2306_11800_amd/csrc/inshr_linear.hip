@@ -199,36 +199,49 @@ __global__ __launch_bounds__(256) void k_tile_stats(TileJobs jobs, WDesc w, u32 
     }
 }
 
-// A thread per row and per column.
-__global__ __launch_bounds__(256) void k_scales(TileJobs jobs)
+// Lines (the rows and columns of both jobs) in blocks of 64; the tiles of a line are dealt to 16 threads, whose results are
+// joined in order (one thread a line read its tiles in 12 us at 1024 x 4096, most of it waiting).
+__global__ __launch_bounds__(1024) void k_scales(TileJobs jobs)
 {
-    u64 i = blockIdx.x * 256ull + threadIdx.x;
+    __shared__ u32 mags[16][64];
+    __shared__ float sums[16][64];
+    const u32 lane = threadIdx.x & 63u, part = threadIdx.x >> 6;
+    u64 block = blockIdx.x;
     for (int q = 0; q < 2; q++) {
         const TileJob &j = jobs.job[q];
         if (!j.src.p) return;
-        if (i < j.src.rows) {
-            if (!j.row_max) return;
-            u32 m = 0u;
-#pragma unroll 16
-            for (u32 t = 0; t < j.col_tiles; t++) m = max(m, gptr(j.row_max)[(u64)t * j.src.rows + i]);
-            float s;
-            scale_of(m, s, j.inv_row[i]);
-            return;
-        }
-        i -= j.src.rows;
-        if (i < j.src.cols) {
-            u32 m = 0u;
-            float sum = 0.0f, s;
-#pragma unroll 8
-            for (u32 t = 0; t < j.row_tiles; t++) {
-                if (j.col_max) m = max(m, gptr(j.col_max)[(u64)t * j.src.cols + i]);
-                if (j.col_sum) sum += gptr(j.col_sum)[(u64)t * j.src.cols + i];
+        for (int by_col = 0; by_col < 2; by_col++) {
+            const u32 lines = by_col ? j.src.cols : j.src.rows, tiles = by_col ? j.row_tiles : j.col_tiles, blocks = (lines + 63u) / 64u;
+            if (block >= blocks) {
+                block -= blocks;
+                continue;
             }
-            if (j.col_max) scale_of(m, s, j.inv_col[i]);
-            if (j.col_sum) j.sum[i] = sum;
+            const u32 line = (u32)block * 64u + lane;
+            const u32 *max_of = by_col ? j.col_max : j.row_max;
+            const float *sum_of = by_col ? j.col_sum : nullptr;
+            u32 m = 0u;
+            float sum = 0.0f;
+            if (line < lines) {
+#pragma unroll 4
+                for (u32 t = part; t < tiles; t += 16u) {
+                    if (max_of) m = max(m, gptr(max_of)[(u64)t * lines + line]);
+                    if (sum_of) sum += gptr(sum_of)[(u64)t * lines + line];
+                }
+            }
+            mags[part][lane] = m;
+            sums[part][lane] = sum;
+            __syncthreads();
+            if (part == 0u && line < lines) {
+                for (u32 t = 1; t < 16u; t++) {
+                    m = max(m, mags[t][lane]);
+                    sum += sums[t][lane];
+                }
+                float s;
+                if (max_of) scale_of(m, s, (by_col ? j.inv_col : j.inv_row)[line]);
+                if (sum_of) j.sum[line] = sum;
+            }
             return;
         }
-        i -= j.src.cols;
     }
 }
 
@@ -500,28 +513,30 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
     for (u32 q = 0; q < (u32)D; q++) fetch(q);
     wait_and_meet<LOADS *(D - 1)>();
     read(even, 0);
-    for (u32 t = 0; t < n_steps; t += 2u) {
+    for (u32 t = 0; t < n_steps; t += 2u) { // (an even number: see cut_of)
         step(even, odd, t);
-        if (t + 1u < n_steps) step(odd, even, t + 1u);
+        step(odd, even, t + 1u);
     }
     // The sums go through LDS, up to 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
-    static_assert(WN == 64, "");
     constexpr int ROWS = WM < 64 ? WM : 64;
+    static_assert(WN % 64 == 0 && WM % ROWS == 0, "");
     float s, inv_w = 1.0f;
     if (!g.inv_b && !g.partial) weight_scale(g.wpart, s, inv_w);
     float *const mine = (float *)lds + wave * (ROWS * 64u); // [ROWS][64], the pieces of 4 of a row in an order of its own
-    const u32 n = n0 + wn + (lane & 7u) * 8u;
 #pragma unroll
-    for (int part = 0; part < WM / ROWS; part++) {
+    for (int part = 0; part < WM / ROWS * (WN / 64); part++) {
+        const int down = part % (WM / ROWS), across = part / (WM / ROWS);
+        const u32 n = n0 + wn + across * 64u + (lane & 7u) * 8u;
         __syncthreads();
 #pragma unroll
         for (u32 i = 0; i < ROWS / 16u; i++)
 #pragma unroll
-            for (u32 j = 0; j < 4u; j++) *(f4 *)(mine + (i * 16u + r16) * 64u + ((j * 4u + (lane >> 4)) ^ r16) * 4u) = acc[part * (ROWS / 16) + i][j];
+            for (u32 j = 0; j < 4u; j++)
+                *(f4 *)(mine + (i * 16u + r16) * 64u + ((j * 4u + (lane >> 4)) ^ r16) * 4u) = acc[down * (ROWS / 16) + i][across * 4 + j];
         __syncthreads();
 #pragma unroll 1
         for (u32 q = 0; q < ROWS / 8u; q++) {
-            const u32 r = q * 8u + (lane >> 3), m = m0 + wm + part * ROWS + r, c = (lane & 7u) * 2u;
+            const u32 r = q * 8u + (lane >> 3), m = m0 + wm + down * ROWS + r, c = (lane & 7u) * 2u;
             if (m >= g.M || n >= g.N) continue;
             const f4 x = *(const f4 *)(mine + r * 64u + (c ^ (r & 15u)) * 4u), y = *(const f4 *)(mine + r * 64u + ((c + 1u) ^ (r & 15u)) * 4u);
             if (g.partial) {
@@ -661,7 +676,7 @@ Cut cut_of(u64 M, u64 N, u64 ld, u32 pairs)
     const u64 tiles = (u64)c.m_tiles * c.n_tiles, steps = ld / KS;
     c.splits = 1;
     while (c.splits < 16u && tiles * c.splits * 2u <= CUS && steps * pairs / (2u * c.splits) >= 8u && steps >= 2u * c.splits) c.splits *= 2u;
-    c.steps = (u32)((steps + c.splits - 1) / c.splits);
+    c.steps = (u32)up((steps + c.splits - 1) / c.splits, 2); // (two sets of operands take turns; `steps` is even, as KT / KS is)
     c.splits = (u32)((steps + c.steps - 1) / c.steps); // (none without a step)
     c.partial = c.splits > 1 ? up(N, 8) * M * c.splits * 4u : 0;
     return c;
@@ -845,13 +860,13 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
     }
     u32 *part = dx ? (u32 *)(c.ws + r.part) : nullptr;
     const u32 grid = t.tiles + (dx ? WMAX_PARTS : 0u);
-    const u64 lines = c.rows + c.n_out + (dw ? c.rows + c.n_in : 0u);
+    const u32 lines = d.row_tiles + d.col_tiles + (dw ? x.row_tiles + x.col_tiles : 0u); // in blocks of 64, as the tiles are
     switch (c.type) {
     case TY_F32: PROF("k_tile_stats", s, k_tile_stats<TY_F32><<<grid, 256, 0, s>>>(t, c.w, part)); break;
     case TY_BF16: PROF("k_tile_stats", s, k_tile_stats<TY_BF16><<<grid, 256, 0, s>>>(t, c.w, part)); break;
     default: PROF("k_tile_stats", s, k_tile_stats<TY_F16><<<grid, 256, 0, s>>>(t, c.w, part)); break;
     }
-    PROF("k_scales", s, k_scales<<<(u32)((lines + 255) / 256), 256, 0, s>>>(t));
+    PROF("k_scales", s, k_scales<<<lines, 1024, 0, s>>>(t));
     if (dx || dw) switch (c.type) {
     case TY_F32: tile_planes<TY_F32>(t, r.dr.count, r.dc.count, s); break;
     case TY_BF16: tile_planes<TY_BF16>(t, r.dr.count, r.dc.count, s); break;
