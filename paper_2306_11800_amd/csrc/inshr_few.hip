@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256) void k_few_pack(Mat x, u32 rows, u32 cols, u32
     }
 }
 
-constexpr u32 AHEAD = 2; // steps whose part of the stream is asked for before one is worked on
+constexpr u32 AHEAD = 1; // steps whose part of the stream is asked for before one is worked on (two: fewer waves, 16 -> 20 us for a token)
 
 // This wave's steps of 128 of the reduction, `every` apart.  SAFE: no load of the stream can lead past its end.
 template <u32 TY, int W, int MT, bool PACKED, bool SAFE>
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
     typedef typename Elem<TY>::type T;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ u64 range[2];
-    __shared__ u32 starts[18];
+    __shared__ u32 starts[17];
     __shared__ __attribute__((aligned(16))) float sums[16 * MT][16], listed[16 * MT][16];
     u32 *table = (u32 *)lds;
     f4 *part = (f4 *)(lds + Table<TY, W>::BYTES);
@@ -315,7 +315,20 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
         const u64 first = (u64)min(n0 + half * 16u, f.n_out) * K;
         const u64 at = f.w.n_outlier ? first_listed(f.w, first, lane & 31u, half) : 0;
         if ((lane & 31u) == 0u) range[half] = at;
-        if (!PACKED) listed_by_wave<TY>(f, __shfl(at, 0), __shfl(at, 32), n0, listed);
+        const u64 lo = __shfl(at, 0), hi = __shfl(at, 32);
+        if (!PACKED) {
+            listed_by_wave<TY>(f, lo, hi, n0, listed);
+        } else if (lane <= 16u && hi > lo) { // where each output's entries begin, relative to lo
+            const u64 first_of = (u64)min(n0 + lane, f.n_out) * K;
+            u32 from = 0u, n = (u32)(hi - lo);
+            while (n) {
+                const u32 half_n = n / 2u;
+                const bool below = gptr(f.w.out_idx)[lo + from + half_n] < first_of;
+                from += below ? half_n + 1u : 0u;
+                n = below ? n - half_n - 1u : half_n;
+            }
+            starts[lane] = from;
+        }
     } else {
         f4 acc[MT] = {};
         if (safe)
@@ -328,7 +341,6 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
     __syncthreads();
     const u64 lo = range[0], hi = range[1];
     const u32 rows = min(f.rows - m0, 16u * MT);
-    if (PACKED && hi > lo) row_starts(f.w, lo, hi, n0, 16u, starts);
     // lane (i, g) of a part holds row i, outputs 4 g .. 4 g + 3
     for (u32 j = threadIdx.x; j < MT * 64u; j += blockDim.x) {
         f4 v = part[j];
@@ -338,7 +350,7 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
     __syncthreads();
     if (PACKED && hi > lo) { // a wave per output; four lanes an entry, eight rows each, four entries a lane at a time
         for (u32 t = wave; t < 16u; t += waves + 1u) {
-            const u32 count = (u32)(hi - lo), from = min(starts[t], count), to = min(starts[t + 1u], count), base = (n0 + t) * K;
+            const u32 from = starts[t], to = starts[t + 1u], base = (n0 + t) * K; // (at most hi - lo)
             const GLOBAL_AS T *x = (const GLOBAL_AS T *)f.turned + (u64)(m0 / TURNED) * K * TURNED + (lane & 3u) * 8u;
             float sum[8] = {};
             for (u32 j0 = from + (lane >> 2); j0 < to; j0 += 64u) {
@@ -544,10 +556,12 @@ struct FewRoom {
 template <u32 TY, int W, int MT, bool PACKED>
 void start_rows(Few &f, hipStream_t s)
 {
-    // As many waves as let all workgroups run at once at 16 waves a CU (a round of workgroups that is partly empty costs
-    // more than longer waves: 688 of 9 waves 31 us, of 5 waves 20), but not more than there are steps for.
-    const u32 groups = (f.n_out + 15u) / 16u * f.row_blocks, per_cu = (groups + 255u) / 256u;
-    u32 waves = per_cu >= 5u ? 2u : 16u / per_cu - 1u;
+    // As many waves as let all workgroups run at once, at 24 waves a CU (16 with two tiles of rows, which take more
+    // registers), but not more than there are steps for.  A token through 4096 x 11008, 688 workgroups: 5 waves each 18.4 us,
+    // 6 16.9, 8 15.6, 10 19.7; 9 waves in two rounds 25.
+    const u32 groups = (f.n_out + 15u) / 16u * f.row_blocks, per_cu = (groups + 255u) / 256u, slots = MT == 1 ? 24u : 16u;
+    u32 waves = per_cu >= slots / 3u ? 2u : slots / per_cu - 1u;
+    waves = waves < 15u ? waves : 15u;
     waves = waves < f.steps ? waves : f.steps;
     PROF("k_few_rows", s, k_few_rows<TY, W, MT, PACKED><<<groups, 64u * (waves + 1u), Table<TY, W>::BYTES + waves * MT * 1024u, s>>>(f));
 }

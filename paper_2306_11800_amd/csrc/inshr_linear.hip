@@ -323,9 +323,22 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
     typedef Table<TY_F16, W> Tab;
     constexpr int ND = (8 * W + 31) / 32;
     __shared__ __attribute__((aligned(16))) u32 table[Tab::BYTES / 4];
+    // a tile of 64 rows x 128 columns (64 for turned planes): four runs a thread (two), asked for before anything else
+    constexpr u32 TILE_C = T ? 64u : 128u, RUNS = TILE_C / 32u;
+    const u32 col_tiles = (w.cols + TILE_C - 1u) / TILE_C;
+    const u64 r0 = blockIdx.x / col_tiles * 64ull;
+    const u32 c0 = blockIdx.x % col_tiles * TILE_C;
+    const bool is_tile = blockIdx.x < tiles;
+    u32 raw[RUNS][ND + 1];
+#pragma unroll
+    for (u32 h = 0; h < RUNS; h++) {
+        const u32 i = threadIdx.x + 256u * h, c = c0 + i % (TILE_C / 8u) * 8u;
+        const u64 r = r0 + i / (TILE_C / 8u);
+        load_words<ND + 1>(w.packed, (r * w.cols + c) * W >> 5, is_tile && r < w.rows && c < w.cols ? w.n_words : 0, raw[h]);
+    }
     float s, inv;
     weight_scale(part, s, inv);
-    if (blockIdx.x >= tiles) {
+    if (!is_tile) {
         for (u64 j = (blockIdx.x - tiles) * 256ull + threadIdx.x; j < w.n_outlier; j += (u64)(gridDim.x - tiles) * 256u) {
             const u32 i = gptr(w.out_idx)[j], r = i / w.cols, c = i - r * w.cols;
             if (r >= w.rows) continue;
@@ -338,24 +351,19 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
         return;
     }
     fill_table<TY_F16, W>(w, table, s);
+    if (threadIdx.x >= Tab::COPIES && threadIdx.x < 2u * Tab::COPIES) table[threadIdx.x] = ONE_MARK; // (this thread's entry)
     __syncthreads();
     const u32 mine = lane_copy<TY_F16, W>();
-    // a tile of 64 rows x 128 columns: four runs a thread
-    constexpr u32 TILE_C = T ? 64u : 128u;
-    const u32 col_tiles = (w.cols + TILE_C - 1u) / TILE_C;
-    const u64 r0 = blockIdx.x / col_tiles * 64ull;
-    const u32 c0 = blockIdx.x % col_tiles * TILE_C;
     __shared__ u32 turned[T ? 64 : 1][65];
 #pragma unroll
-    for (u32 h = 0; h < TILE_C / 32u; h++) {
+    for (u32 h = 0; h < RUNS; h++) {
         const u32 i = threadIdx.x + 256u * h, run = i % (TILE_C / 8u), c = c0 + run * 8u;
         const u64 r = r0 + i / (TILE_C / 8u);
         const u32 left = r < w.rows && c < w.cols ? w.cols - c : 0u;
-        u32 raw[ND + 1], d[ND + 1];
-        const u64 bit = (r * w.cols + c) * W;
-        load_words<ND + 1>(w.packed, bit >> 5, left ? w.n_words : 0, raw);
+        u32 d[ND + 1];
+        const u32 shift = (u32)((r * w.cols + c) * W) & 31u;
 #pragma unroll
-        for (int q = 0; q < ND; q++) d[q] = __builtin_amdgcn_alignbit(raw[q + 1], raw[q], (u32)bit & 31u);
+        for (int q = 0; q < ND; q++) d[q] = __builtin_amdgcn_alignbit(raw[h][q + 1], raw[h][q], shift);
         d[ND] = 0u;
         u32 e[8][2];
         u32 at_one = 0u; // protected places
@@ -363,11 +371,11 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
         for (int q = 0; q < 8; q++) {
             look_up<TY_F16, W>((const char *)table, mine, d, q, e[q]);
             if ((u32)q >= left) e[q][0] = 0u;
-            if (!T) at_one |= (symbol_of<W>(d, q) == 1u && (u32)q < left ? 1u : 0u) << q;
+            at_one |= (e[q][0] == ONE_MARK ? 1u : 0u) << q;
         }
         if (T) {
 #pragma unroll
-            for (int q = 0; q < 8; q++) turned[i / (TILE_C / 8u)][run * 8u + q] = symbol_of<W>(d, q) == 1u && (u32)q < left ? ONE_MARK : e[q][0];
+            for (int q = 0; q < 8; q++) turned[i / (TILE_C / 8u)][run * 8u + q] = e[q][0];
         } else if (r < w.rows && c < (u32)ld) {
             store_entries<P>(e, at_one, dst + plane_at(r, c, ld), plane);
         }

@@ -79,12 +79,6 @@ __device__ __forceinline__ void look_up(const char *table, u32 mine, const u32 *
         e[0] = *(const u32 *)p;
     }
 }
-template <int W>
-__device__ __forceinline__ u32 symbol_of(const u32 *d, int j)
-{
-    const int bit = j * W, at = bit >> 5, off = bit & 31;
-    return (off + W > 32 ? __builtin_amdgcn_alignbit(d[at + 1], d[at], (u32)off) : d[at] >> off) & ((1u << W) - 1u);
-}
 __device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
