@@ -12,7 +12,7 @@
 //                           fp16      the centre scaled by a power of two as two fp16 numbers (22 bits), two instructions
 //                           fp32      centre and activation as three bfloat16 numbers each (all 24 bits), the six products
 //                                     that matter
-//   weight [n_in][n_out]  k_few_split: a thread keeps the sums of 8 consecutive outputs and walks down a part of the rows of
+//   weight [n_in][n_out]  k_few_split: a thread keeps the sums of 16 or 8 consecutive outputs and walks down a part of the rows of
 //                         the weight; k_few_join adds the parts.  fp32 throughout, one multiplication per weight and row of
 //                         activations, which is why it takes up to FEW_SPLIT rows.
 // All sums are taken in a fixed order.  Protected values are 0 in the table and are added from the list.
@@ -120,18 +120,17 @@ __device__ __forceinline__ u64 first_listed(const WDesc &w, u64 index, u32 half_
     return lo;
 }
 
-// Where the entries of each stored row begin: starts[t] for rows r0 + t, t = 0 .. n, relative to lo.  lo .. hi: the entries of
-// these rows.  By the whole workgroup; a barrier has to follow.  (A list that is not in order may leave places unset: they
-// are read as at most hi - lo.)
-__device__ __forceinline__ void row_starts(const WDesc &w, u64 lo, u64 hi, u32 r0, u32 n, u32 *starts)
+// Where entries of `index` and above begin among the count ones from lo on, relative to lo (and so at most count).
+__device__ __forceinline__ u32 starts_at(const WDesc &w, u64 lo, u32 count, u64 index)
 {
-    const u32 count = (u32)(hi - lo);
-    for (u32 j = threadIdx.x; j <= count; j += blockDim.x) {
-        // (clamped: a list that is not in order must not lead out of the array)
-        const u32 before = j == 0u ? 0u : min(gptr(w.out_idx)[lo + j - 1u] / w.cols - r0 + 1u, n + 1u);
-        const u32 here = j == count ? n : min(gptr(w.out_idx)[lo + j] / w.cols - r0, n);
-        for (u32 t = before; t <= here; t++) starts[t] = j;
+    u32 from = 0u;
+    while (count) {
+        const u32 half = count / 2u;
+        const bool below = gptr(w.out_idx)[lo + from + half] < index;
+        from += below ? half + 1u : 0u;
+        count = below ? count - half - 1u : half;
     }
+    return from;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -319,15 +318,7 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
         if (!PACKED) {
             listed_by_wave<TY>(f, lo, hi, n0, listed);
         } else if (lane <= 16u && hi > lo) { // where each output's entries begin, relative to lo
-            const u64 first_of = (u64)min(n0 + lane, f.n_out) * K;
-            u32 from = 0u, n = (u32)(hi - lo);
-            while (n) {
-                const u32 half_n = n / 2u;
-                const bool below = gptr(f.w.out_idx)[lo + from + half_n] < first_of;
-                from += below ? half_n + 1u : 0u;
-                n = below ? n - half_n - 1u : half_n;
-            }
-            starts[lane] = from;
+            starts[lane] = starts_at(f.w, lo, (u32)(hi - lo), (u64)min(n0 + lane, f.n_out) * K);
         }
     } else {
         f4 acc[MT] = {};
@@ -395,100 +386,119 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
 // ------------------------------------------------------------------------------------------
 // weight [n_in][n_out]
 // ------------------------------------------------------------------------------------------
-constexpr u32 SPLIT_COLS = 2048; // outputs of a workgroup: 256 threads, eight each
+// Consecutive outputs of a thread, 256 of which walk down the rows together.  (Runs of 16 take 4 loads where two of 8 take
+// 6, but make half the workgroups: one token through 1024 x 4096 13.1 us with 16 and 11.8 with 8, through 4096 x 11008 29.8
+// and 35.6.  Four rows' sums of 16 outputs do not fit into the registers.)
+inline u32 split_run(u32 rows, u32 n_in, u32 n_out) { return rows == 1u && (u64)n_in * n_out >= (16ull << 20) ? 16u : 8u; }
 constexpr u32 SPLIT_DEPTH = 64;  // most rows of the weight that it walks down
 
-// Rows blockIdx.x % splits * depth .. of the weight.  Table: the values themselves.
-template <u32 TY, int W, int M>
-__global__ __launch_bounds__(256) void k_few_split(Few f)
+// Rows blockIdx.x % splits * depth .. of the weight.  Table: the values themselves.  Four waves walk down the rows; the
+// fifth looks up where the protected entries of each row are meanwhile.
+template <u32 TY, int W, int M, u32 R>
+__global__ __launch_bounds__(320) void k_few_split(Few f)
 {
     typedef typename Elem<TY>::type T;
     typedef Table<TY_BF16, W> Tab; // (one word an entry, as there)
-    constexpr int ND = (8 * W + 31) / 32;
+    constexpr u32 COLS = 256u * R, STAGE = 1024, THREADS = 320;
+    constexpr int ND = (R * W + 31) / 32;
     constexpr u32 ROWS = 4; // rows asked for before one is worked on
     __shared__ __attribute__((aligned(16))) u32 table[Tab::BYTES / 4];
     __shared__ float xs[SPLIT_DEPTH][M];
-    __shared__ float extra[M][SPLIT_COLS];
-    __shared__ u32 starts[SPLIT_DEPTH + 2];
+    __shared__ float extra[M][COLS];
+    __shared__ u32 starts[SPLIT_DEPTH + 1], stage_col[STAGE];
+    __shared__ float stage_val[STAGE];
     __shared__ u64 range[2];
-    const u32 split = blockIdx.x % f.splits, n0 = blockIdx.x / f.splits * SPLIT_COLS, ka = split * f.depth, kn = min(f.depth, f.n_in - ka);
-    const u32 run = threadIdx.x * 8u, n = n0 + run;
+    const u32 split = blockIdx.x % f.splits, n0 = blockIdx.x / f.splits * COLS, ka = split * f.depth, kn = min(f.depth, f.n_in - ka);
+    const u32 tid = threadIdx.x, run = tid * R, n = n0 + run;
+    const bool walks = tid < 256u && n < f.n_out;
     const u64 first_bit = ((u64)ka * f.n_out + n) * W, row_bits = (u64)f.n_out * W;
     u32 raw[ROWS][ND + 1];
     auto ask = [&](u32 j, u32 *d) { // row j of the part
         const u64 bit = first_bit + j * row_bits;
-        load_words<ND + 1, false>(f.w.packed, bit >> 5, n < f.n_out && j < kn ? f.w.n_words : 0, d);
+        load_words<ND + 1>(f.w.packed, bit >> 5, walks && j < kn ? f.w.n_words : 0, d);
     };
 #pragma unroll
     for (u32 j = 0; j < ROWS; j++) ask(j, raw[j]);
-    for (u32 i = threadIdx.x; i < kn * M; i += 256u)
+    for (u32 i = tid; i < kn * M; i += THREADS)
         xs[i / M][i % M] = i % M < f.rows ? Elem<TY>::get(((const GLOBAL_AS T *)f.x.p)[(u64)(i % M) * f.x.stride + ka + i / M]) : 0.0f;
-    for (u32 i = threadIdx.x; i < (1u << W) * Tab::COPIES; i += 256u) table[i] = __float_as_uint(symbol_value(f.w, i / Tab::COPIES));
+    for (u32 i = tid; i < (1u << W) * Tab::COPIES; i += THREADS) table[i] = __float_as_uint(symbol_value(f.w, i / Tab::COPIES));
     const bool any = f.w.n_outlier != 0;
-    if (any) {
-        for (u32 i = threadIdx.x; i < M * SPLIT_COLS; i += 256u) extra[i / SPLIT_COLS][i % SPLIT_COLS] = 0.0f;
-        if (threadIdx.x >= 192u) {
-            const u32 lane = threadIdx.x & 63u, half = lane >> 5;
-            const u64 at = first_listed(f.w, (u64)(ka + half * kn) * f.n_out, lane & 31u, half);
-            if ((lane & 31u) == 0u) range[half] = at;
-        }
-    }
+    if (any)
+        for (u32 i = tid; i < M * COLS; i += THREADS) extra[i / COLS][i % COLS] = 0.0f;
     __syncthreads();
-    const u64 lo = any ? range[0] : 0, hi = any ? range[1] : 0;
-    if (hi > lo) row_starts(f.w, lo, hi, ka, kn, starts);
-    const u32 mine = lane_copy<TY_BF16, W>();
-    float acc[M][8] = {};
-    for (u32 j0 = 0; j0 < kn; j0 += ROWS) {
+    float acc[M][R] = {};
+    if (tid >= 256u) {
+        const u32 lane = tid & 63u, half = lane >> 5;
+        const u64 at = any ? first_listed(f.w, (u64)(ka + half * kn) * f.n_out, lane & 31u, half) : 0;
+        if ((lane & 31u) == 0u) range[half] = at;
+        const u64 lo = __shfl(at, 0), hi = __shfl(at, 32);
+        if (hi > lo)
+            for (u32 t = lane; t <= kn; t += 64u) starts[t] = starts_at(f.w, lo, (u32)(hi - lo), (u64)(ka + t) * f.n_out);
+    } else {
+        const u32 mine = lane_copy<TY_BF16, W>();
+        for (u32 j0 = 0; j0 < kn; j0 += ROWS) {
 #pragma unroll
-        for (u32 q = 0; q < ROWS; q++) {
-            const u32 j = j0 + q;
-            if (j >= kn) break;
-            const u32 shift = (u32)(first_bit + j * row_bits) & 31u;
-            u32 d[ND + 1];
+            for (u32 q = 0; q < ROWS; q++) {
+                const u32 j = j0 + q;
+                if (j >= kn) break;
+                const u32 shift = (u32)(first_bit + j * row_bits) & 31u;
+                u32 d[ND + 1];
 #pragma unroll
-            for (int t = 0; t < ND; t++) d[t] = __builtin_amdgcn_alignbit(raw[q][t + 1], raw[q][t], shift);
-            d[ND] = 0u;
-            ask(j + ROWS, raw[q]);
-            float x[M];
+                for (int t = 0; t < ND; t++) d[t] = __builtin_amdgcn_alignbit(raw[q][t + 1], raw[q][t], shift);
+                d[ND] = 0u;
+                ask(j + ROWS, raw[q]);
+                float x[M];
 #pragma unroll
-            for (int m = 0; m < M; m++) x[m] = xs[j][m];
+                for (int m = 0; m < M; m++) x[m] = xs[j][m];
 #pragma unroll
-            for (int t = 0; t < 8; t++) {
-                u32 e[2];
-                look_up<TY_BF16, W>((const char *)table, mine, d, t, e);
+                for (int t = 0; t < (int)R; t++) {
+                    u32 e[2];
+                    look_up<TY_BF16, W>((const char *)table, mine, d, t, e);
 #pragma unroll
-                for (int m = 0; m < M; m++) acc[m][t] = fmaf(x[m], __uint_as_float(e[0]), acc[m][t]);
+                    for (int m = 0; m < M; m++) acc[m][t] = fmaf(x[m], __uint_as_float(e[0]), acc[m][t]);
+                }
             }
         }
     }
     __syncthreads();
-    // the protected values row by row: a row has an output once
+    // the protected values row by row, as a row has an output once; a part of the list at a time in LDS
+    const u64 lo = range[0], hi = range[1];
     if (hi > lo) {
-        for (u32 j = 0; j < kn; j++) {
-            const u32 count = (u32)(hi - lo), to = min(starts[j + 1u], count);
-            for (u32 q = min(starts[j], count) + threadIdx.x; q < to; q += 256u) {
-                const u32 c = gptr(f.w.out_idx)[lo + q] - (ka + j) * f.n_out - n0;
-                if (c >= SPLIT_COLS || c + n0 >= f.n_out) continue;
-                const float v = protected_value(f.w, lo + q);
-#pragma unroll
-                for (int m = 0; m < M; m++) extra[m][c] = fmaf(xs[j][m], v, extra[m][c]);
+        const u32 count = (u32)(hi - lo);
+        u32 j = 0; // the first row that is not done
+        for (u32 s0 = 0; s0 < count; s0 += STAGE) {
+            const u32 s1 = min(count, s0 + STAGE);
+            for (u32 i = s0 + tid; i < s1; i += THREADS) {
+                stage_col[i - s0] = gptr(f.w.out_idx)[lo + i];
+                stage_val[i - s0] = protected_value(f.w, lo + i);
             }
             __syncthreads();
+            for (; j < kn; j++) {
+                const u32 from = max(starts[j], s0), to = min(starts[j + 1u], s1);
+                for (u32 i = from + tid; i < to; i += THREADS) {
+                    const u32 c = stage_col[i - s0] - (ka + j) * f.n_out - n0;
+                    if (c >= COLS || c + n0 >= f.n_out) continue;
+#pragma unroll
+                    for (int m = 0; m < M; m++) extra[m][c] = fmaf(xs[j][m], stage_val[i - s0], extra[m][c]);
+                }
+                __syncthreads();
+                if (starts[j + 1u] > s1) break; // (the rest of the row is in the next part)
+            }
         }
     }
-    if (n >= f.n_out) return;
+    if (!walks) return;
 #pragma unroll
     for (int m = 0; m < M; m++) {
         if ((u32)m >= f.rows) break;
-        f4 a, b;
-#pragma unroll
-        for (int t = 0; t < 4; t++) {
-            a[t] = acc[m][t] + (any ? extra[m][run + t] : 0.0f);
-            b[t] = acc[m][t + 4] + (any ? extra[m][run + t + 4] : 0.0f);
-        }
         float *to = f.partial + ((u64)split * f.rows + m) * f.n8 + n;
-        *(f4 *)to = a;
-        *(f4 *)(to + 4) = b;
+#pragma unroll
+        for (u32 q = 0; q < R; q += 4u) {
+            if (n + q >= f.n8) break;
+            f4 a;
+#pragma unroll
+            for (u32 t = 0; t < 4u; t++) a[t] = acc[m][q + t] + (any ? extra[m][run + q + t] : 0.0f);
+            *(f4 *)(to + q) = a;
+        }
     }
 }
 
@@ -545,7 +555,7 @@ struct FewRoom {
             return;
         }
         // about 768 workgroups (three a CU) where the weight has 4 rows for each at least, SPLIT_DEPTH at most
-        const u32 blocks = (n_out + SPLIT_COLS - 1u) / SPLIT_COLS;
+        const u32 cols = 256u * split_run((u32)rows, n_in, n_out), blocks = (n_out + cols - 1u) / cols;
         depth = (u32)(((u64)n_in * blocks + 767u) / 768u);
         depth = depth < 4u ? 4u : depth > SPLIT_DEPTH ? SPLIT_DEPTH : depth;
         splits = (n_in + depth - 1u) / depth;
@@ -594,13 +604,15 @@ void start_few(Few &f, const LinearCall &c, hipStream_t s)
     f.splits = r.splits;
     f.depth = r.depth;
     f.n8 = (f.n_out + 7u) / 8u * 8u;
-    const u32 grid = r.splits * ((f.n_out + SPLIT_COLS - 1u) / SPLIT_COLS);
+    const u32 run = split_run(f.rows, f.n_in, f.n_out), grid = r.splits * ((f.n_out + 256u * run - 1u) / (256u * run));
     with_width(f.w.w, [&](auto w) {
         constexpr int W = decltype(w)::value;
-        if (f.rows == 1u)
-            PROF("k_few_split", s, k_few_split<TY, W, 1><<<grid, 256, 0, s>>>(f));
+        if (f.rows > 1u)
+            PROF("k_few_split", s, k_few_split<TY, W, (int)FEW_SPLIT, 8><<<grid, 320, 0, s>>>(f));
+        else if (run == 16u)
+            PROF("k_few_split", s, k_few_split<TY, W, 1, 16><<<grid, 320, 0, s>>>(f));
         else
-            PROF("k_few_split", s, k_few_split<TY, W, (int)FEW_SPLIT><<<grid, 256, 0, s>>>(f));
+            PROF("k_few_split", s, k_few_split<TY, W, 1, 8><<<grid, 320, 0, s>>>(f));
     });
     PROF("k_few_join", s, k_few_join<TY><<<f.rows * ((f.n_out + 63u) / 64u), 256, 0, s>>>(f));
 }

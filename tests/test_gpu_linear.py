@@ -182,6 +182,19 @@ def test_protected_lists(ctx, protected):
             check_grad(ctx, layer, W, x, rows_of(rng, rows, n_out, dtype), None)
 
 
+@pytest.mark.parametrize("in_out", [False, True], ids=["oi", "io"])
+def test_long_protected_lists(ctx, in_out):
+    """More entries for a workgroup than it holds at a time, in few long rows and in many."""
+    rng = np.random.default_rng(17)
+    for n_in, n_out, protected in ((40, 3000, 120_000), (300, 70, 21_000), (2000, 40, 40_000)):
+        codes = A.Codes(rng, n_in * n_out, 8, protected)
+        layer = api.QuantizedLayer(codes.quantized(api, DEV), n_out, n_in, in_out)
+        W = torch.from_numpy(codes.values)
+        W = W.view(n_in, n_out).t() if in_out else W.view(n_out, n_in)
+        for rows, dtype in ((1, F32), (3, BF16), (20, F16), (90, BF16)):
+            check_linear(ctx, layer, W, rows_of(rng, rows, n_in, dtype), None)
+
+
 def test_magnitudes_far_apart(ctx):
     """Rows of very different size, a weight whose protected values are 2^20 times its centres, values near the ends of
     the fp32 range: every row keeps its own precision."""
