@@ -525,9 +525,9 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
         step(even, odd, t);
         step(odd, even, t + 1u);
     }
-    // The sums go through LDS, up to 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
-    constexpr int ROWS = WM < 64 ? WM : 64;
-    static_assert(WN % 64 == 0 && WM % ROWS == 0, "");
+    // The sums go through LDS, 32 or 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
+    constexpr int MOST = (int)(D * SLOT / (WAVES * 128)), ROWS = WM <= MOST && WM <= 64 ? WM : MOST >= 64 ? 64 : 32; // (64 floats a row)
+    static_assert(WN % 64 == 0 && WM % ROWS == 0 && ROWS <= MOST, "every wave has its rows in LDS");
     float s, inv_w = 1.0f;
     if (!g.inv_b && !g.partial) weight_scale(g.wpart, s, inv_w);
     float *const mine = (float *)lds + wave * (ROWS * 64u); // [ROWS][64], the pieces of 4 of a row in an order of its own

@@ -107,9 +107,10 @@ def test_shapes(ctx, shape, in_out, dtype):
 
 
 @pytest.mark.parametrize("rows,n_in,n_out,in_out", [(2100, 130, 8200, False), (2049, 200, 8000, True), (70, 4200, 4100, False),
-                                                    (66, 4097, 4500, True), (260, 9000, 70, False), (4100, 66, 130, True)])
+                                                    (66, 4097, 4500, True), (260, 9000, 70, False), (4100, 66, 130, True),
+                                                    (4096, 70, 4096, False), (2048, 70, 11008, False)])
 def test_large_shapes(ctx, rows, n_in, n_out, in_out):
-    """Many tiles, or few with a long reduction."""
+    """Many tiles of each size, or few with a long reduction."""
     rng = np.random.default_rng(rows)
     for dtype in (BF16, F32):
         layer, W, x, r = case(rng, rows, n_in, n_out, 16, dtype, "silu", in_out, residual=True, protected=5000)
