@@ -479,7 +479,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
         from[j] = (u64)block * 16u * g.ld;
     }
     const u32 step0 = split * g.steps, n_steps = min(g.steps, g.ld / KS - step0) * g.pairs;
-    u64 k = step0 * (16u * KS); // blocks of a row follow each other
+    u64 k = (u64)step0 * (16u * KS); // blocks of a row follow each other
     u32 pass = 0, asked = 0;
     auto fetch = [&](u32 slot) { // the next step's rows; past the last step once more the last one's, which nobody reads
         const _Float16 *a = g.a + ((g.pa >> pass) & 1u) * g.plane_a + k, *b = g.b + ((g.pb >> pass) & 1u) * g.plane_b + k;
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
     for (u32 q = 0; q < (u32)D; q++) fetch(q);
     wait_and_meet<LOADS *(D - 1)>();
     read(even, 0);
-    for (u32 t = 0; t < n_steps; t += 2u) { // (an even number: see cut_of)
+    for (u32 t = 0; t < n_steps; t += 2u) { // (an even number: cut_of, and KT / KS is even)
         step(even, odd, t);
         step(odd, even, t + 1u);
     }
@@ -682,10 +682,10 @@ Cut cut_of(u64 M, u64 N, u64 ld, u32 pairs)
     c.m_tiles = (u32)(up(M, KIND_M[c.kind]) / KIND_M[c.kind]);
     c.n_tiles = (u32)(up(N, KIND_N[c.kind]) / KIND_N[c.kind]);
     const u64 tiles = (u64)c.m_tiles * c.n_tiles, steps = ld / KS;
-    c.splits = 1;
-    while (c.splits < 16u && tiles * c.splits * 2u <= CUS && steps * pairs / (2u * c.splits) >= 8u && steps >= 2u * c.splits) c.splits *= 2u;
-    c.steps = (u32)up((steps + c.splits - 1) / c.splits, 2); // (two sets of operands take turns; `steps` is even, as KT / KS is)
-    c.splits = (u32)((steps + c.steps - 1) / c.steps); // (none without a step)
+    // as many as there are CUs for the tiles, with eight steps of a tile each at least
+    const u64 most = std::min(std::min<u64>(CUS / tiles, 16u), std::min(steps * pairs / 8u, steps / 2u));
+    c.steps = (u32)up((steps + most - (most > 0)) / std::max<u64>(most, 1u), pairs & 1u ? 2 : 1); // (two sets of operands take turns)
+    c.splits = (u32)((steps + c.steps - 1) / c.steps);
     c.partial = c.splits > 1 ? up(N, 8) * M * c.splits * 4u : 0;
     return c;
 }
