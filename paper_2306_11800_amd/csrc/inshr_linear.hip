@@ -422,15 +422,16 @@ __device__ __forceinline__ void to_lds(const _Float16 *from, u32 lane, _Float16 
     __builtin_amdgcn_global_load_lds((const GLOBAL_AS u32 *)from + lane * 4u, (LDS_AS u32 *)to, 16, 0, 0);
 }
 
-// The scaled sums of row m, columns n .. n + 7, to where they belong.
+// The scaled sums of row m, columns n .. n + 7, to where they belong.  (The scales are powers of two, and the exponents are
+// added first: a row near the upper end of fp32 times a small weight would overflow with one of them alone.)
 template <u32 TY>
 __device__ __forceinline__ void scaled8(const Gemm &g, u32 m, u32 n, float (&v)[8], float inv_w)
 {
-    const float inv_a = gptr(g.inv_a)[m];
+    const int e = exponent_of(gptr(g.inv_a)[m]);
     float b[8];
     if (g.inv_b) load8<TY_F32>(gptr(g.inv_b) + n, min(g.N - n, 8u), b);
 #pragma unroll
-    for (int t = 0; t < 8; t++) v[t] = v[t] * inv_a * (g.inv_b ? b[t] : inv_w);
+    for (int t = 0; t < 8; t++) v[t] = __builtin_ldexpf(v[t], e + exponent_of(g.inv_b ? b[t] : inv_w));
     finish8<TY>(g.end, m, n, v);
 }
 

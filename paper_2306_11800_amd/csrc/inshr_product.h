@@ -21,6 +21,7 @@ __device__ __forceinline__ void scale_of(u32 mag, float &s, float &inv)
     s = __uint_as_float(sb << 23);
     inv = __uint_as_float((254u - sb) << 23);
 }
+__device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23) - 127; } // of a power of two
 __device__ __forceinline__ u32 mag_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 __device__ __forceinline__ u32 wave_max_u(u32 v)
 {

@@ -213,6 +213,22 @@ def test_magnitudes_far_apart(ctx):
             check_linear(ctx, layer, W, x, None)
 
 
+def test_rows_near_the_ends_of_the_range(ctx):
+    """Rows and weights whose own scales leave the fp32 range while their products do not."""
+    rng = np.random.default_rng(18)
+    for e, scale in ((120, 2.0 ** -30), (-110, 2.0 ** 30)):
+        for rows, in_out in ((3, False), (3, True), (120, False), (120, True)):
+            codes = A.Codes(rng, 200 * 72, 16, 30, scale=scale)
+            layer = api.QuantizedLayer(codes.quantized(api, DEV), 72, 200, in_out)
+            W = torch.from_numpy(codes.values)
+            W = W.view(200, 72).t() if in_out else W.view(72, 200)
+            for dtype in (F32, BF16):
+                x = rows_of(rng, rows, 200, dtype).clamp_(-4, 4)
+                check_linear(ctx, layer, W, x * 2.0 ** e, None)
+                dy = rows_of(rng, rows, 72, dtype).clamp_(-4, 4)
+                check_grad(ctx, layer, W, x * scale, dy * 2.0 ** e, None)
+
+
 def test_non_finite_rows(ctx):
     rng = np.random.default_rng(9)
     for dtype in (F32, BF16, F16):
