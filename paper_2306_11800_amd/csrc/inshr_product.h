@@ -80,6 +80,12 @@ __device__ __forceinline__ void act_of(float (&v)[N], u32 act)
         break;
     }
 }
+// a for the slopes' polynomials: past `end` the slope is 0 or 1 (to 2^-100), and powers of a would outrun the exponential,
+// which ends at 2^126; NaN stays
+__device__ __forceinline__ float within(float a, float end)
+{
+    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(a, -end), end);
+}
 // v times the slope at a
 template <int N>
 __device__ __forceinline__ void act_grad(float (&v)[N], const float (&a)[N], u32 act)
@@ -99,16 +105,16 @@ __device__ __forceinline__ void act_grad(float (&v)[N], const float (&a)[N], u32
 #pragma unroll
         for (int i = 0; i < N; i++) {
             float rest;
-            const float s = logistic(bend(a[i]), rest);
-            v[i] *= s + a[i] * s * rest * 1.59576912160573071f * (1.0f + 0.134145f * a[i] * a[i]);
+            const float x = within(a[i], 16.0f), s = logistic(bend(x), rest);
+            v[i] *= s + x * s * rest * 1.59576912160573071f * (1.0f + 0.134145f * x * x);
         }
         break;
     case ACT_SILU:
 #pragma unroll
         for (int i = 0; i < N; i++) {
             float rest;
-            const float s = logistic(a[i], rest);
-            v[i] *= s * (1.0f + a[i] * rest);
+            const float x = within(a[i], 120.0f), s = logistic(x, rest);
+            v[i] *= s * (1.0f + x * rest);
         }
         break;
     }

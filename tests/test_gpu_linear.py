@@ -138,6 +138,26 @@ def test_activations(ctx, act, dtype):
         check_grad(ctx, layer, W, x, rows_of(rng, rows, 72, dtype), pre)
 
 
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_slopes_far_out(ctx, act):
+    """Where an activation is straight its slope is 0 or 1, however large the values below it; NaN stays NaN."""
+    rng = np.random.default_rng(19)
+    for dtype, far in ((F32, (20.0, 130.0, 1e3, 1e12, 1e20, 3e38)), (BF16, (20.0, 1e20, 3e38)), (F16, (20.0, 1e3, 65504.0))):
+        layer, W, x, _ = case(rng, 70, 64, 40, 16, dtype, act)
+        dy = rows_of(rng, 70, 40, dtype)
+        pre = torch.tensor(far, device=DEV).to(dtype)[torch.from_numpy(rng.integers(0, len(far), (70, 40))).to(DEV)]
+        pre = torch.where(torch.from_numpy(rng.random((70, 40)) < 0.5).to(DEV), pre, -pre)
+        _, dw, db = ctx.linear_grad(layer, x, dy, pre)
+        d = torch.where(pre.cpu() > 0, f64(dy), 0.0)  # (silu's slope is off 0 and 1 by 20 e^-20 = 4e-8 < 2^-24 at +-20)
+        off = 2.0 ** -20 * f64(dy).abs()
+        want, S = d.t() @ f64(x), d.abs().t() @ f64(x).abs()
+        near(dw, want, A.tol_sum(S, 70, F32, d.abs().amax(0)[:, None] * f64(x).abs().amax(0)[None]) + off.t() @ f64(x).abs() + A.TINY[F32])
+        near(db, d.sum(0), 70 * 2.0 ** -24 * d.abs().sum(0) + off.sum(0) + A.TINY[F32])
+        pre[3, 5] = float("nan")
+        db = ctx.linear_grad(layer, x, dy, pre, want_dx=False, want_dw=False)[2]
+        assert bool(torch.isnan(db[5])) and int(torch.isnan(db).sum()) == 1
+
+
 @pytest.mark.parametrize("gap,at", [(1, 0), (3, 1), (8, 0), (64, 5), (5, 8)])
 def test_strides_and_alignment(ctx, gap, at):
     rng = np.random.default_rng(gap)
