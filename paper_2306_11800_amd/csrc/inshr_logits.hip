@@ -284,6 +284,9 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
         for (u32 i = k + tid; i < n; i += BLOCK) add1(rest, logit_of((u32)(cand[i] >> 32)), c2);
         n = k;
     }
+    // (candidates stand in the order in which they were found, which is another one every time: those that are not listed
+    // are added up in the order of their places)
+    __shared__ float late[BLOCK];
     if (tid < n) {
         const u64 own = cand[tid];
         u32 place = 0u;
@@ -294,10 +297,12 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
             gptr(index)[r * k + place] = (int)at;
             gptr(value)[r * k + place] = Elem<TY>::get(p[at]); // (of the two zeros the one that is there)
         } else {
-            add1(rest, logit_of((u32)(own >> 32)), c2);
+            late[place] = logit_of((u32)(own >> 32));
         }
     }
     if (tail) {
+        __syncthreads();
+        if (tid >= k && tid < n) add1(rest, late[tid], c2);
         put_sum(rest, LOG2E * inv_T, room);
         __syncthreads();
         if (tid >= 64u) return;

@@ -89,6 +89,17 @@ def test_top_with_nan_and_infinity(ctx):
     assert bool(torch.isfinite(top.tail[3])) and torch.equal(top.index[3].long(), plain_top(z[3:].cpu().double(), 4, 1.0)[0][0].to(DEV))
 
 
+def test_the_same_every_time(ctx):
+    rng = np.random.default_rng(20)
+    for rows, vocab, k in ((600, 5000, 60), (20, 40000, 200)):
+        z = logits_of(rng, rows, vocab, F32)
+        z[::3, 100:900] = 2.0  # more equal ones than there are places
+        a, b = (ctx.top_logits(z, k, 1.5) for _ in range(2))
+        (la, sa), (lb, sb) = (ctx.distill(z * 0.5, a) for _ in range(2))
+        assert torch.equal(a.index, b.index) and torch.equal(a.value, b.value) and torch.equal(a.tail, b.tail)
+        assert torch.equal(la, lb) and torch.equal(sa, sb)
+
+
 def plain_distill(z, index, value, tail, T, g):
     """(loss, gradient, sum of the magnitudes behind the loss) in 64 bits, row by row, from the definitions."""
     rows, vocab = z.shape
