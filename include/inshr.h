@@ -409,7 +409,7 @@ typedef struct {
  *   residual  [rows][n_out] or NULL; may be y itself (same address and stride)
  *   y         [rows][n_out]
  *   pre       [rows][n_out] or NULL: receives x W^T + bias, which inshr_linear_grad wants
- * y and pre share no memory with each other or with x.
+ * y and pre share no memory with each other, with x or (but for y as above) with the residual.
  * Sums are held in fp32; a result is rounded once, `pre` on its own.  The factors are fp16 numbers scaled
  * by powers of two (one per row of x, one for the weight), in two parts each for fp32 results, one and two
  * for fp16, one each for bfloat16: what that takes from a product is 2^-22, 2^-22 and 2^-11 of it, or 2^-40
@@ -421,7 +421,7 @@ typedef struct {
  * that it enters NaN, listed indices outside the weight are left out, and with a list that is not the
  * stream's ascending one the results are undefined.
  * INSHR_E_ARG: a NULL or misaligned pointer, an unknown type or activation, dimensions out of range,
- * weight.n != n_out * n_in, an output stride below its columns; INSHR_E_CONFIG: the codes' bits / bins;
+ * weight.n != n_out * n_in, an output stride below its columns, an output that begins where it may not; INSHR_E_CONFIG: the codes' bits / bins;
  * INSHR_E_CAPACITY: workspace_bytes too small. */
 int inshr_linear_bound(const inshr_layer *layer, uint64_t rows, uint64_t *workspace_bytes);
 int inshr_linear(inshr_ctx *ctx, const inshr_layer *layer, inshr_matrix x, inshr_matrix residual, inshr_matrix y,

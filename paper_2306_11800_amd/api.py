@@ -988,12 +988,17 @@ class Context:
             raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor [rows, {cols}] on {self._device}")
         return shape[0], type_
 
+    def _own(self, layer):
+        if layer.device != self._device:
+            raise ValueError(f"the layer is on {layer.device}, the context on {self._device}")
+
     def linear(self, layer: QuantizedLayer, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
                out: Optional[torch.Tensor] = None, want_pre: bool = False):
         """act(x W^T + bias) + residual of x [rows, n_in] (float32, bfloat16 or float16; rows may lie apart), in x's
         type; with want_pre also x W^T + bias, which linear_grad takes.  out may be the residual itself.  Returns
         after enqueueing."""
         rows, type_ = self._rows_of(x, layer.n_in, "x")
+        self._own(layer)
         dev, dt, n_out = self._device, x.dtype, layer.n_out
         cx = _matrix(x, rows, layer.n_in, dt, dev, "x")
         cr = _matrix(residual, rows, n_out, dt, dev, "residual")
@@ -1020,6 +1025,7 @@ class Context:
         the layout of the weight (what quantize_sens takes), dbias float32 [n_out]; None for what is not wanted.  x is
         needed for dw, pre for every activation but none.  Returns after enqueueing."""
         rows, type_ = self._rows_of(dy, layer.n_out, "dy")
+        self._own(layer)
         dev, dt, n_in, n_out = self._device, dy.dtype, layer.n_in, layer.n_out
         if want_dw and x is None:
             raise ValueError("dw needs x")

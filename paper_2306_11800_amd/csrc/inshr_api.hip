@@ -2505,6 +2505,8 @@ int inshr_linear(inshr_ctx *c, const inshr_layer *layer, inshr_matrix x, inshr_m
         !matrix_ok(y, layer->type, layer->n_out, true, true) || !matrix_ok(pre, layer->type, layer->n_out, false, true))
         return INSHR_E_ARG;
     if (residual.data == y.data && residual.stride != y.stride) return INSHR_E_ARG;
+    if (y.data == x.data || y.data == pre.data) return INSHR_E_ARG;
+    if (pre.data && (pre.data == x.data || pre.data == residual.data)) return INSHR_E_ARG;
     rc = workspace_ok(c, "inshr_linear", workspace, workspace_bytes,
                       linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->weight.n_outlier != 0));
     if (rc) return rc;
@@ -2552,6 +2554,8 @@ int inshr_linear_grad(inshr_ctx *c, const inshr_layer *layer, inshr_matrix x, in
                  !matrix_ok(pre, layer->type, layer->n_out, bent, false) || !matrix_ok(dx, layer->type, layer->n_in, false, true)))
         return INSHR_E_ARG;
     if (!aligned(dw, 4) || !aligned(dbias, 4)) return INSHR_E_ARG;
+    for (const void *result : {(const void *)dx.data, (const void *)dw, (const void *)dbias})
+        if (rows && result && (result == x.data || result == dy.data || result == pre.data)) return INSHR_E_ARG;
     rc = workspace_ok(c, "inshr_linear_grad", workspace, workspace_bytes,
                       linear_grad_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->activation,
                                         dx.data != nullptr, dw != nullptr));

@@ -77,6 +77,12 @@ def test_tensors(ctx):
                dict(out=torch.zeros((2, 8)))):
         with pytest.raises(ValueError, match="(residual|out) must"):
             ctx.linear(l, x, **kw)
+    far = layer()
+    far.device = torch.device("meta")
+    with pytest.raises(ValueError, match="the layer is on meta"):
+        ctx.linear(far, x)
+    with pytest.raises(ValueError, match="the layer is on meta"):
+        ctx.linear_grad(far, x, torch.zeros((3, 8)))
     dy = torch.zeros((3, 8))
     with pytest.raises(ValueError, match="dw needs x"):
         ctx.linear_grad(l, None, dy)

@@ -373,6 +373,7 @@ def test_refusals(ctx):
     assert call(x=api.CMatrix(x.data_ptr() + 1, 64)) == -1           # between elements
     assert call(y=m(y, 31)) == -1 and call(pre=m(y, 31)) == -1       # rows that overlap
     assert call(r=m(y, 64)) == -1                                     # the result's place, other rows
+    assert call(y=m(x, 64)) == -1 and call(pre=m(y)) == -1 and call(pre=m(x, 64)) == -1 and call(pre=m(r)) == -1
     assert call(rows=(1 << 22) + 1) == -1
     if need.value:
         assert call(rows=200, b=need.value - 1) == -4
@@ -382,6 +383,7 @@ def test_refusals(ctx):
         h, C.byref(c), m(x), m(r), pre, dx, dw, db, 4, ws.data_ptr(), 0)
     assert grad() == -1                                               # nothing wanted
     assert grad(dx=m(x, 63)) == -1 and grad(dw=x.data_ptr() + 2) == -1
+    assert grad(dx=m(r, 64)) == -1 and grad(dx=m(x)) == -1 and grad(dw=r.data_ptr()) == -1
     ctx.sync()
 
 
