@@ -415,6 +415,11 @@ struct Gemm {
     float *partial;          // [splits][M][n8] their sums; NULL: one workgroup has the whole reduction
     u32 n8;                  // N rounded up to 8
 };
+struct Gemms { // one product, or two that share a launch (the other's type is fp32, or the same)
+    Gemm g[2];
+    u32 first;      // workgroups of the first
+    u32 join_first; // workgroups of k_join for the first
+};
 
 // A block of 1024 bytes from device memory to LDS without registers in between.
 __device__ __forceinline__ void to_lds(const _Float16 *from, u32 lane, _Float16 *to)
@@ -422,7 +427,7 @@ __device__ __forceinline__ void to_lds(const _Float16 *from, u32 lane, _Float16 
     __builtin_amdgcn_global_load_lds((const GLOBAL_AS u32 *)from + lane * 4u, (LDS_AS u32 *)to, 16, 0, 0);
 }
 
-// The scaled sums of row m, columns n .. n + 7, to where they belong.  (The scales are powers of two, and the exponents are
+// The scaled sums of row m, columns n .. n + 7, to where they belong, as elements of TY or of fp32.  (The scales are powers of two, and the exponents are
 // added first: a row near the upper end of fp32 times a small weight would overflow with one of them alone.)
 template <u32 TY>
 __device__ __forceinline__ void scaled8(const Gemm &g, u32 m, u32 n, float (&v)[8], float inv_w)
@@ -432,7 +437,10 @@ __device__ __forceinline__ void scaled8(const Gemm &g, u32 m, u32 n, float (&v)[
     if (g.inv_b) load8<TY_F32>(gptr(g.inv_b) + n, min(g.N - n, 8u), b);
 #pragma unroll
     for (int t = 0; t < 8; t++) v[t] = __builtin_ldexpf(v[t], e + exponent_of(g.inv_b ? b[t] : inv_w));
-    finish8<TY>(g.end, m, n, v);
+    if (TY == TY_F32 || g.type == TY)
+        finish8<TY>(g.end, m, n, v);
+    else
+        store8<TY_F32>((GLOBAL_AS float *)g.end.out.p + (u64)m * g.end.out.stride + n, min(g.N - n, 8u), v);
 }
 
 // Waits until at most N loads to LDS of this wave are on their way and all its reads of LDS have come, then for the others.
@@ -449,8 +457,11 @@ __device__ __forceinline__ void wait_and_meet()
 template <u32 TY, int BM, int BN, int WM, int WN, int D>
 // (Eight waves: with four, one a SIMD, the compiler keeps the sums in accumulation registers and moves them to and fro
 // around every product, 0.5 us a step of 128 x 128.)
-__global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
+__global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemms both)
 {
+    const bool second = blockIdx.x >= both.first;
+    const Gemm g = both.g[second];
+    const u32 block = blockIdx.x - (second ? both.first : 0u);
     constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TM = WM / 16, TN = WN / 16;
     constexpr int LOADS = (BM + BN) / 16 / WAVES; // of 16 rows each, per wave and step
     constexpr u32 SLOT = (BM + BN) * KS;
@@ -460,7 +471,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
     // Workgroups go to the eight XCDs in turn; each XCD gets a run of them, of one split first, whose blocks it finds in its
     // own L2 ...
     const u32 tiles = g.m_tiles * g.n_tiles, all = tiles * g.splits, per = (all + 7u) / 8u;
-    const u32 full = all - (per - 1u) * 8u, xcd = blockIdx.x & 7u, at = blockIdx.x >> 3; // the first `full` XCDs have `per`
+    const u32 full = all - (per - 1u) * 8u, xcd = block & 7u, at = block >> 3; // the first `full` XCDs have `per`
     u32 id = xcd < full ? xcd * per + at : full * per + (xcd - full) * (per - 1u) + at;
     const u32 split = id / tiles;
     id -= split * tiles;
@@ -476,8 +487,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
         const u32 r = (wave * LOADS + j) * 16u;
         is_b[j] = r >= (u32)BM;
         // (blocks past the last are the last: their results are not stored)
-        const u32 block = is_b[j] ? min(n0 + r - BM, g.N - 1u) / 16u : min(m0 + r, g.M - 1u) / 16u;
-        from[j] = (u64)block * 16u * g.ld;
+        const u32 sixteen = is_b[j] ? min(n0 + r - BM, g.N - 1u) / 16u : min(m0 + r, g.M - 1u) / 16u;
+        from[j] = (u64)sixteen * 16u * g.ld;
     }
     const u32 step0 = split * g.steps, n_steps = min(g.steps, g.ld / KS - step0) * g.pairs;
     u64 k = (u64)step0 * (16u * KS); // blocks of a row follow each other
@@ -522,7 +533,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
     for (u32 q = 0; q < (u32)D; q++) fetch(q);
     wait_and_meet<LOADS *(D - 1)>();
     read(even, 0);
-    for (u32 t = 0; t < n_steps; t += 2u) { // (an even number: cut_of, and KT / KS is even)
+    for (u32 t = 0; t < n_steps; t += 2u) { // (an even number: see cuts_of)
         step(even, odd, t);
         step(odd, even, t + 1u);
     }
@@ -560,28 +571,29 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemm g)
     }
 }
 
-// The sums of the splits, in their order.
+// The sums of the splits, in their order: eight results a thread.
 template <u32 TY>
-__global__ __launch_bounds__(256) void k_join(Gemm g)
+__global__ __launch_bounds__(256) void k_join(Gemms both)
 {
+    const bool second = blockIdx.x >= both.join_first;
+    const Gemm g = both.g[second];
+    const u64 i = (blockIdx.x - (second ? both.join_first : 0u)) * 256ull + threadIdx.x;
     float s, inv_w = 1.0f;
     if (!g.inv_b) weight_scale(g.wpart, s, inv_w);
-    const u32 parts = g.n8 / 8u;
-    const u64 all = (u64)g.M * parts;
-    for (u64 i = blockIdx.x * 256ull + threadIdx.x; i < all; i += (u64)gridDim.x * 256u) {
-        const u32 m = (u32)(i / parts), n = (u32)(i - (u64)m * parts) * 8u;
-        float v[8] = {};
-        for (u32 q = 0; q < g.splits; q++) {
-            const GLOBAL_AS f4 *p = (const GLOBAL_AS f4 *)(gptr(g.partial) + ((u64)q * g.M + m) * g.n8 + n);
-            const f4 x = p[0], y = p[1];
+    const u32 parts = g.n8 / 8u, m = (u32)(i / parts), n = (u32)(i - (u64)m * parts) * 8u;
+    if (m >= g.M) return;
+    float v[8] = {};
+#pragma unroll 4
+    for (u32 q = 0; q < g.splits; q++) {
+        const GLOBAL_AS f4 *p = (const GLOBAL_AS f4 *)(gptr(g.partial) + ((u64)q * g.M + m) * g.n8 + n);
+        const f4 x = p[0], y = p[1];
 #pragma unroll
-            for (int t = 0; t < 4; t++) {
-                v[t] += x[t];
-                v[t + 4] += y[t];
-            }
+        for (int t = 0; t < 4; t++) {
+            v[t] += x[t];
+            v[t + 4] += y[t];
         }
-        scaled8<TY>(g, m, n, v, inv_w);
     }
+    scaled8<TY>(g, m, n, v, inv_w);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -658,78 +670,151 @@ void weight_planes(const WDesc &w, bool along, const Planes &p, char *ws, u64 pa
     });
 }
 
-// How a product is cut: tiles of 256 x 256, 128 x 256 or 128 x 128, whichever rounds of 256 workgroups take the least time
-// (a step of a tile measured 0.91, 0.52 and 0.30 us on a full chip), and with tiles too few for the chip the reduction
-// among several workgroups.
+// How products that share a launch are cut: tiles of 256 x 256, 128 x 256 or 128 x 128, one size for both, and where the
+// tiles are too few for the chip the reduction of a tile among several workgroups.
+struct Shape { // M == 0: no such product
+    u64 M = 0, N = 0, ld = 0;
+    u32 pairs = 1;
+};
 struct Cut {
-    int kind;
     u32 m_tiles, n_tiles, splits, steps;
     u64 partial; // bytes
 };
+struct Cuts {
+    int kind;
+    Cut c[2];
+};
 constexpr u32 CUS = 256;
-constexpr u32 KIND_M[3] = {256, 128, 128}, KIND_N[3] = {256, 256, 128}, KIND_TIME[3] = {91, 52, 30};
-Cut cut_of(u64 M, u64 N, u64 ld, u32 pairs)
+constexpr u32 KIND_M[3] = {256, 128, 128}, KIND_N[3] = {256, 256, 128};
+// Measured, in 0.01 us: a step of a tile on a full chip; what a workgroup takes beside its steps (the first loads, the
+// results), and a launch of k_join; and 4 bytes of fp32 sums written and read again, in 2^-20 of it
+constexpr u32 KIND_TIME[3] = {91, 52, 30}, KIND_FIXED[3] = {900, 500, 300}, JOIN_TIME = 350, SUM_TIME = 210;
+
+// The time until all workgroups are done, the ones that take longer first: n0 that take t0 each and n1 that take t1.
+u64 time_of(u32 n0, u32 t0, u32 n1, u32 t1)
 {
-    Cut c;
-    u64 best = ~0ull;
-    for (int kind = 0; kind < 3; kind++) {
-        const u64 tiles = up(M, KIND_M[kind]) / KIND_M[kind] * (up(N, KIND_N[kind]) / KIND_N[kind]);
-        const u64 time = up(tiles, CUS) / CUS * KIND_TIME[kind];
-        if (time < best) {
-            best = time;
-            c.kind = kind;
-        }
+    if (t0 < t1) {
+        std::swap(n0, n1);
+        std::swap(t0, t1);
     }
-    c.m_tiles = (u32)(up(M, KIND_M[c.kind]) / KIND_M[c.kind]);
-    c.n_tiles = (u32)(up(N, KIND_N[c.kind]) / KIND_N[c.kind]);
-    const u64 tiles = (u64)c.m_tiles * c.n_tiles, steps = ld / KS;
-    // as many as there are CUs for the tiles, with eight steps of a tile each at least
-    const u64 most = std::min(std::min<u64>(CUS / tiles, 16u), std::min(steps * pairs / 8u, steps / 2u));
-    c.steps = (u32)up((steps + most - (most > 0)) / std::max<u64>(most, 1u), pairs & 1u ? 2 : 1); // (two sets of operands take turns)
-    c.splits = (u32)((steps + c.steps - 1) / c.steps);
-    c.partial = c.splits > 1 ? up(N, 8) * M * c.splits * 4u : 0;
-    return c;
+    const u32 busy = n0 % CUS, free = CUS - busy; // `busy` CUs have longer ones `until`, the others until `full`
+    const u64 full = (u64)(n0 / CUS) * t0, until = full + (busy ? t0 : 0);
+    const u32 beside = busy ? t0 / t1 : 0; // shorter ones that end beside a last longer one
+    if ((u64)n1 <= (u64)beside * free) return std::max(until, full + (u64)((n1 + free - 1) / free) * t1);
+    n1 -= beside * free;
+    const u32 rounds = n1 / CUS, left = n1 % CUS;
+    const u64 end = until + (u64)rounds * t1;
+    if (left == 0) return end;
+    return left > free ? end + t1 : std::max(end, full + (u64)(beside + rounds + 1) * t1);
+}
+
+// Numbers of workgroups for a tile that are looked at.
+constexpr u32 MOST_SPLITS = 16, SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, MOST_SPLITS};
+struct Choice {
+    u32 groups, time, extra;
+    Cut c;
+};
+// Those of a product, `MOST_SPLITS` at most; returns how many.
+u32 choices_of(const Shape &x, int kind, Choice *to)
+{
+    Choice o = {};
+    o.c.splits = 1;
+    o.time = 1; // (no such product: no workgroups)
+    if (x.M == 0) {
+        to[0] = o;
+        return 1;
+    }
+    o.c.m_tiles = (u32)(up(x.M, KIND_M[kind]) / KIND_M[kind]);
+    o.c.n_tiles = (u32)(up(x.N, KIND_N[kind]) / KIND_N[kind]);
+    const u32 tiles = o.c.m_tiles * o.c.n_tiles, steps = (u32)(x.ld / KS);
+    u32 n = 0;
+    for (u32 want : SPLITS) {
+        if (want > 1 && (tiles * want > 2 * CUS || steps * x.pairs < 8 * want)) break; // (eight steps each)
+        // (two sets of operands take turns: an even number of steps and passes; `steps` is even, as KT / KS is)
+        o.c.steps = (u32)up((steps + want - 1) / want, x.pairs & 1u ? 2 : 1);
+        o.c.splits = (steps + o.c.steps - 1) / o.c.steps;
+        o.c.partial = o.c.splits > 1 ? up(x.N, 8) * x.M * o.c.splits * 4u : 0;
+        o.groups = tiles * o.c.splits;
+        o.time = KIND_FIXED[kind] + o.c.steps * x.pairs * KIND_TIME[kind];
+        o.extra = (u32)(o.c.partial / 4u * SUM_TIME >> 20) + (o.c.partial ? JOIN_TIME : 0u);
+        if (n == 0 || o.c.steps < to[n - 1].c.steps) to[n++] = o;
+    }
+    return n;
+}
+
+Cuts cuts_of(const Shape &a, const Shape &b)
+{
+    Cuts best = {};
+    u64 least = ~0ull;
+    for (int kind = 0; kind < 3; kind++) {
+        Choice x[MOST_SPLITS], y[MOST_SPLITS];
+        const u32 nx = choices_of(a, kind, x), ny = choices_of(b, kind, y);
+        for (u32 i = 0; i < nx; i++)
+            for (u32 j = 0; j < ny; j++) {
+                const u64 extra = x[i].extra + y[j].extra - (x[i].extra && y[j].extra ? JOIN_TIME : 0u); // (one launch)
+                if (((u64)x[i].groups * x[i].time + (u64)y[j].groups * y[j].time) / CUS + extra >= least) continue;
+                const u64 time = time_of(x[i].groups, x[i].time, y[j].groups, y[j].time) + extra;
+                if (time >= least) continue;
+                least = time;
+                best = {kind, {x[i].c, y[j].c}};
+            }
+    }
+    return best;
 }
 
 template <u32 TY>
-void product_of(const Gemm &g, const Cut &c, hipStream_t s)
+void products_of(const Gemms &g, int kind, u32 grid, u32 join, hipStream_t s)
 {
-    const u32 grid = c.m_tiles * c.n_tiles * c.splits;
-    switch (c.kind) {
+    switch (kind) {
     case 0: PROF("k_product", s, k_product<TY, 256, 256, 128, 64, 4><<<grid, 512, 0, s>>>(g)); break;
     case 1: PROF("k_product", s, k_product<TY, 128, 256, 64, 64, 4><<<grid, 512, 0, s>>>(g)); break;
     default: PROF("k_product", s, k_product<TY, 128, 128, 32, 64, 8><<<grid, 512, 0, s>>>(g)); break;
     }
-    if (c.splits > 1) {
-        const u64 all = (u64)g.M * (g.n8 / 8u), blocks = (all + 255) / 256;
-        PROF("k_join", s, k_join<TY><<<(u32)(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(g));
-    }
+    if (join) PROF("k_join", s, k_join<TY><<<join, 256, 0, s>>>(g));
 }
 
-void product(Gemm g, const Planes &a, const Planes &b, u64 partial, char *ws, hipStream_t s)
+// Where a product's operands and sums are.
+void lay_out(Gemm &g, const Planes &a, const Planes &b, const Cut &c, u64 partial, char *ws)
 {
     g.a = (const _Float16 *)(ws + a.off);
     g.b = (const _Float16 *)(ws + b.off);
     g.plane_a = a.plane;
     g.plane_b = b.plane;
     g.ld = (u32)a.ld;
+    g.inv_a = (const float *)(ws + a.inv);
     // (smallest terms first) l h, h l, h h
-    g.pairs = 0;
-    g.pa = g.pb = 0;
     if (a.count > 1) g.pa |= 1u << g.pairs++;
     if (b.count > 1) g.pb |= 1u << g.pairs++;
     g.pairs++;
-    const Cut c = cut_of(g.M, g.N, a.ld, g.pairs);
     g.m_tiles = c.m_tiles;
     g.n_tiles = c.n_tiles;
     g.splits = c.splits;
     g.steps = c.steps;
     g.n8 = (u32)up(g.N, 8);
-    g.partial = c.splits > 1 ? (float *)(ws + partial) : nullptr;
-    switch (g.type) {
-    case TY_F32: product_of<TY_F32>(g, c, s); break;
-    case TY_BF16: product_of<TY_BF16>(g, c, s); break;
-    default: product_of<TY_F16>(g, c, s); break;
+    g.partial = c.partial ? (float *)(ws + partial) : nullptr;
+}
+// One product (b NULL) or two, whose results have this type or, the second's, fp32.  The one whose workgroups take longer
+// goes first.
+void products(const Gemm &a, const Gemm *b, u32 type, int kind, hipStream_t s)
+{
+    Gemms g = {};
+    const bool turn = b && (u64)b->steps * b->pairs > (u64)a.steps * a.pairs;
+    g.g[0] = turn ? *b : a;
+    if (b) g.g[1] = turn ? a : *b;
+    u32 grid = 0, join = 0;
+    for (int j = 0; j < (b ? 2 : 1); j++) {
+        const Gemm &x = g.g[j];
+        grid += x.m_tiles * x.n_tiles * x.splits;
+        join += x.partial ? (u32)(((u64)x.M * (x.n8 / 8u) + 255u) / 256u) : 0u;
+        if (j == 0) {
+            g.first = grid;
+            g.join_first = join;
+        }
+    }
+    switch (type) {
+    case TY_F32: products_of<TY_F32>(g, kind, grid, join, s); break;
+    case TY_BF16: products_of<TY_BF16>(g, kind, grid, join, s); break;
+    default: products_of<TY_F16>(g, kind, grid, join, s); break;
     }
 }
 
@@ -740,43 +825,48 @@ u32 planes_w(u32 type) { return type == TY_BF16 ? 1u : 2u; }
 struct LinearRoom {
     Planes x, w;
     u64 part, partial, bytes;
+    Cuts cuts;
     LinearRoom(u64 rows, u32 n_in, u32 n_out, u32 type)
     {
         Room r;
         x = planes_for(r, rows, n_in, planes_x(type));
         w = planes_for(r, n_out, n_in, planes_w(type));
         part = r.take(WMAX_PARTS * 4u);
-        partial = r.take(cut_of(rows, n_out, x.ld, x.count + w.count - 1).partial);
+        cuts = cuts_of({rows, n_out, x.ld, x.count + w.count - 1}, {});
+        partial = r.take(cuts.c[0].partial);
         bytes = r.at;
     }
 };
 struct GradRoom {
-    u64 part = 0, partial = 0, bytes = 0;
+    u64 part = 0, partial[2] = {0, 0}, bytes = 0;
     u64 row_max = 0, col_max = 0, col_sum = 0, x_max = 0;
     Planes dr = {}, w = {}, dc = {}, xc = {};
-    GradRoom(u64 rows, u32 n_in, u32 n_out, u32 type, u32 act, bool dx, bool dw)
+    Cuts cuts;
+    GradRoom(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw)
     {
         Room r;
         const u64 row_tiles = up(rows, 64) / 64, col_tiles = up(n_out, 64) / 64;
         // d is what it is in its type, or, below an activation, an fp32 number
         const u32 dt = act != ACT_NONE ? TY_F32 : type;
         col_sum = r.take(row_tiles * n_out * 4u);
+        const u32 d_count = type == TY_BF16 ? 1u : planes_x(dt), w_count = planes_w(type), dc_count = planes_x(dt), x_count = planes_x(type);
+        // (cut as if both were wanted, so that a result does not depend on whether the other one is)
+        const u64 of_rows = up(rows, KT), m = in_out ? n_in : n_out, n = in_out ? n_out : n_in;
+        cuts = cuts_of({rows, n_in, up(n_out, KT), d_count + w_count - 1}, {m, n, of_rows, dc_count + x_count - 1});
         if (dx) {
-            dr = planes_for(r, rows, n_out, type == TY_BF16 ? 1u : planes_x(dt));
-            w = planes_for(r, n_in, n_out, planes_w(type));
+            dr = planes_for(r, rows, n_out, d_count);
+            w = planes_for(r, n_in, n_out, w_count);
             part = r.take(WMAX_PARTS * 4u);
             row_max = r.take(col_tiles * rows * 4u);
+            partial[0] = r.take(cuts.c[0].partial);
         }
         if (dw) { // (fp32 results)
-            dc = planes_for(r, n_out, rows, planes_x(dt));
-            xc = planes_for(r, n_in, rows, planes_x(type));
+            dc = planes_for(r, n_out, rows, dc_count);
+            xc = planes_for(r, n_in, rows, x_count);
             col_max = r.take(row_tiles * n_out * 4u);
             x_max = r.take(row_tiles * n_in * 4u);
+            partial[1] = r.take(cuts.c[1].partial);
         }
-        // (the two products take turns)
-        u64 most = dx ? cut_of(rows, n_in, dr.ld, dr.count + w.count - 1).partial : 0;
-        if (dw) most = std::max(most, std::max(cut_of(n_out, n_in, dc.ld, dc.count + xc.count - 1).partial, cut_of(n_in, n_out, dc.ld, dc.count + xc.count - 1).partial));
-        partial = r.take(most);
         bytes = r.at;
     }
 };
@@ -801,7 +891,7 @@ u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, bool liste
 }
 u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw)
 {
-    return rows ? GradRoom(rows, n_in, n_out, type, act, dx, dw).bytes : 0;
+    return rows ? GradRoom(rows, n_in, n_out, in_out, type, act, dx, dw).bytes : 0;
 }
 
 hipError_t launch_linear(const LinearCall &c, hipStream_t s)
@@ -814,11 +904,11 @@ hipError_t launch_linear(const LinearCall &c, hipStream_t s)
     Gemm g = {};
     g.M = (u32)c.rows;
     g.N = c.n_out;
-    g.inv_a = (const float *)(c.ws + r.x.inv);
     g.wpart = (const u32 *)(c.ws + r.part);
     g.end = {c.bias, c.residual, c.y, c.pre, c.n_out, c.act};
     g.type = c.type;
-    product(g, r.x, r.w, r.partial, c.ws, s);
+    lay_out(g, r.x, r.w, r.cuts.c[0], r.partial, c.ws);
+    products(g, nullptr, c.type, r.cuts.kind, s);
     return hipGetLastError();
 }
 
@@ -834,7 +924,7 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
         if (c.db) PROF("k_zero", s, k_zero<<<64, 256, 0, s>>>(c.db, c.n_out));
         return hipGetLastError();
     }
-    const GradRoom r(c.rows, c.n_in, c.n_out, c.type, c.act, c.dx.p != nullptr, c.dw != nullptr);
+    const GradRoom r(c.rows, c.n_in, c.n_out, c.in_out, c.type, c.act, c.dx.p != nullptr, c.dw != nullptr);
     const bool dx = c.dx.p != nullptr, dw = c.dw != nullptr;
     TileJobs t = {};
     TileJob &d = t.job[0], &x = t.job[1];
@@ -881,28 +971,29 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
     case TY_BF16: tile_planes<TY_BF16>(t, r.dr.count, r.dc.count, s); break;
     default: tile_planes<TY_F16>(t, r.dr.count, r.dc.count, s); break;
     }
+    Gemm gx = {}, gw = {};
     if (dx) {
         weight_planes(c.w, c.in_out, r.w, c.ws, r.part, s);
-        Gemm g = {};
-        g.M = (u32)c.rows;
-        g.N = c.n_in;
-        g.inv_a = (const float *)(c.ws + r.dr.inv);
-        g.wpart = (const u32 *)(c.ws + r.part);
-        g.end = {nullptr, {}, c.dx, {}, c.n_in, ACT_NONE};
-        g.type = c.type;
-        product(g, r.dr, r.w, r.partial, c.ws, s);
+        gx.M = (u32)c.rows;
+        gx.N = c.n_in;
+        gx.wpart = (const u32 *)(c.ws + r.part);
+        gx.end = {nullptr, {}, c.dx, {}, c.n_in, ACT_NONE};
+        gx.type = c.type;
+        lay_out(gx, r.dr, r.w, r.cuts.c[0], r.partial[0], c.ws);
     }
     if (dw) {
         const Planes &a = c.in_out ? r.xc : r.dc, &b = c.in_out ? r.dc : r.xc;
-        Gemm g = {};
-        g.M = c.in_out ? c.n_in : c.n_out;
-        g.N = c.in_out ? c.n_out : c.n_in;
-        g.inv_a = (const float *)(c.ws + a.inv);
-        g.inv_b = (const float *)(c.ws + b.inv);
-        g.end = {nullptr, {}, {c.dw, g.N}, {}, g.N, ACT_NONE};
-        g.type = TY_F32;
-        product(g, a, b, r.partial, c.ws, s);
+        gw.M = c.in_out ? c.n_in : c.n_out;
+        gw.N = c.in_out ? c.n_out : c.n_in;
+        gw.inv_b = (const float *)(c.ws + b.inv);
+        gw.end = {nullptr, {}, {c.dw, gw.N}, {}, gw.N, ACT_NONE};
+        gw.type = TY_F32;
+        lay_out(gw, a, b, r.cuts.c[1], r.partial[1], c.ws);
     }
+    if (dx)
+        products(gx, dw ? &gw : nullptr, c.type, r.cuts.kind, s);
+    else if (dw)
+        products(gw, nullptr, TY_F32, r.cuts.kind, s);
     return hipGetLastError();
 }
 
