@@ -71,22 +71,24 @@ __device__ __forceinline__ void put_planes(const float (&v)[8], float s, _Float1
     if (P > 1) *(h8 *)(at + plane) = lo;
 }
 
-// One workgroup per row, read twice; the first WMAX_PARTS workgroups look through the weight's values instead.
+struct RowPlanes {
+    PlaneSrc src;
+    _Float16 *dst;
+    u64 plane;
+    float *inv;
+    u32 ld, type;
+};
+
+// Row r, by a workgroup of 256, which reads it twice.
 template <u32 TY, int P>
-__global__ __launch_bounds__(256) void k_row_planes(PlaneSrc src, _Float16 *__restrict__ dst, u64 plane, u32 Cp, float *__restrict__ inv_out,
-                                                    WDesc w, u32 *__restrict__ part)
+__device__ __forceinline__ void row_planes(const RowPlanes &j, u64 r)
 {
     typedef typename Elem<TY>::type T;
-    if (blockIdx.x < WMAX_PARTS) {
-        weight_max_part(w, blockIdx.x, part);
-        return;
-    }
-    const u64 r = blockIdx.x - WMAX_PARTS;
-    const GLOBAL_AS T *p = (const GLOBAL_AS T *)src.p + r * src.stride;
+    const GLOBAL_AS T *p = (const GLOBAL_AS T *)j.src.p + r * j.src.stride;
     __shared__ u32 red[4];
     u32 m = 0u;
-    for (u32 c = threadIdx.x * 8u; c < src.cols; c += 2048u) {
-        const Raw8<TY> x = load_raw8<TY>(p + c, src.cols - c);
+    for (u32 c = threadIdx.x * 8u; c < j.src.cols; c += 2048u) {
+        const Raw8<TY> x = load_raw8<TY>(p + c, j.src.cols - c);
 #pragma unroll
         for (int i = 0; i < 8; i++) m = max(m, finite_mag(x[i]));
     }
@@ -95,12 +97,22 @@ __global__ __launch_bounds__(256) void k_row_planes(PlaneSrc src, _Float16 *__re
     __syncthreads();
     float s, inv;
     scale_of(max(max(red[0], red[1]), max(red[2], red[3])), s, inv);
-    if (threadIdx.x == 0) inv_out[r] = inv;
-    for (u32 c = threadIdx.x * 8u; c < Cp; c += 2048u) {
+    if (threadIdx.x == 0) j.inv[r] = inv;
+    for (u32 c = threadIdx.x * 8u; c < j.ld; c += 2048u) {
         float v[8];
-        load8<TY>(p + c, c < src.cols ? src.cols - c : 0u, v);
-        put_planes<P>(v, s, dst + plane_at(r, c, Cp), plane);
+        load8<TY>(p + c, c < j.src.cols ? j.src.cols - c : 0u, v);
+        put_planes<P>(v, s, j.dst + plane_at(r, c, j.ld), j.plane);
     }
+}
+
+// The rows, and in the first WMAX_PARTS workgroups the weight's largest values.
+template <u32 TY, int P>
+__global__ __launch_bounds__(256) void k_row_planes(RowPlanes j, WDesc w, u32 *__restrict__ part)
+{
+    if (blockIdx.x < WMAX_PARTS)
+        weight_max_part(w, blockIdx.x, part);
+    else
+        row_planes<TY, P>(j, blockIdx.x - WMAX_PARTS);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -199,51 +211,49 @@ __global__ __launch_bounds__(256) void k_tile_stats(TileJobs jobs, WDesc w, u32 
     }
 }
 
-// Lines (the rows and columns of both jobs) in blocks of 64; the tiles of a line are dealt to 16 threads, whose results are
-// joined in order (one thread a line read its tiles in 12 us at 1024 x 4096, most of it waiting).
-__global__ __launch_bounds__(1024) void k_scales(TileJobs jobs)
+// Lines (the rows and columns of both jobs) in blocks of 16, by a workgroup of 256: the tiles of a line are dealt to 16
+// threads, whose results are joined in order (one thread a line read its tiles in 12 us at 1024 x 4096, most of it waiting).
+constexpr u32 LINES = 16;
+__device__ __forceinline__ u32 line_blocks(const TileJobs &jobs, u32 which) // rows and columns of the first, then of the second
 {
-    __shared__ u32 mags[16][64];
-    __shared__ float sums[16][64];
-    const u32 lane = threadIdx.x & 63u, part = threadIdx.x >> 6;
-    u64 block = blockIdx.x;
-    for (int q = 0; q < 2; q++) {
-        const TileJob &j = jobs.job[q];
-        if (!j.src.p) return;
-        for (int by_col = 0; by_col < 2; by_col++) {
-            const u32 lines = by_col ? j.src.cols : j.src.rows, tiles = by_col ? j.row_tiles : j.col_tiles, blocks = (lines + 63u) / 64u;
-            if (block >= blocks) {
-                block -= blocks;
-                continue;
-            }
-            const u32 line = (u32)block * 64u + lane;
-            const u32 *max_of = by_col ? j.col_max : j.row_max;
-            const float *sum_of = by_col ? j.col_sum : nullptr;
-            u32 m = 0u;
-            float sum = 0.0f;
-            if (line < lines) {
+    const TileJob &j = jobs.job[which >> 1];
+    return j.src.p ? ((which & 1u ? j.src.cols : j.src.rows) + LINES - 1u) / LINES : 0u;
+}
+__device__ __forceinline__ void join_lines(const TileJobs &jobs, u32 block)
+{
+    __shared__ u32 mags[16][LINES];
+    __shared__ float sums[16][LINES];
+    const u32 lane = threadIdx.x % LINES, part = threadIdx.x / LINES;
+    u32 which = 0u;
+    for (; which < 3u && block >= line_blocks(jobs, which); which++) block -= line_blocks(jobs, which);
+    const TileJob &j = jobs.job[which >> 1];
+    const bool by_col = which & 1u;
+    const u32 lines = by_col ? j.src.cols : j.src.rows, tiles = by_col ? j.row_tiles : j.col_tiles, line = block * LINES + lane;
+    const u32 *max_of = by_col ? j.col_max : j.row_max;
+    const float *sum_of = by_col ? j.col_sum : nullptr;
+    u32 m = 0u;
+    float sum = 0.0f;
+    if (line < lines) {
 #pragma unroll 4
-                for (u32 t = part; t < tiles; t += 16u) {
-                    if (max_of) m = max(m, gptr(max_of)[(u64)t * lines + line]);
-                    if (sum_of) sum += gptr(sum_of)[(u64)t * lines + line];
-                }
-            }
-            mags[part][lane] = m;
-            sums[part][lane] = sum;
-            __syncthreads();
-            if (part == 0u && line < lines) {
-                for (u32 t = 1; t < 16u; t++) {
-                    m = max(m, mags[t][lane]);
-                    sum += sums[t][lane];
-                }
-                float s;
-                if (max_of) scale_of(m, s, (by_col ? j.inv_col : j.inv_row)[line]);
-                if (sum_of) j.sum[line] = sum;
-            }
-            return;
+        for (u32 t = part; t < tiles; t += 16u) {
+            if (max_of) m = max(m, gptr(max_of)[(u64)t * lines + line]);
+            if (sum_of) sum += gptr(sum_of)[(u64)t * lines + line];
         }
     }
+    mags[part][lane] = m;
+    sums[part][lane] = sum;
+    __syncthreads();
+    if (part == 0u && line < lines) {
+        for (u32 t = 1; t < 16u; t++) {
+            m = max(m, mags[t][lane]);
+            sum += sums[t][lane];
+        }
+        float s;
+        if (max_of) scale_of(m, s, (by_col ? j.inv_col : j.inv_row)[line]);
+        if (sum_of) j.sum[line] = sum;
+    }
 }
+__global__ __launch_bounds__(256) void k_scales(TileJobs jobs) { join_lines(jobs, blockIdx.x); }
 
 // P1, P2: planes by row and by column (of both jobs)
 template <u32 TY, int PR, int PC0, int PC1>
@@ -314,21 +324,63 @@ __device__ __forceinline__ void store_entries(const u32 (&e)[8][2], u32 skip, _F
 }
 constexpr u32 ONE_MARK = 0xFC00FC00u; // (minus infinity twice: no entry has a high part that is infinite and one that is left over)
 
+// What shares the launch with the weight: rows of activations, or the lines of a gradient's scales.
+struct Beside {
+    RowPlanes rows;
+    TileJobs jobs;
+    u32 n_rows, n_lines; // workgroups
+};
+constexpr u32 SHORT_LIST = 4096; // protected values that every workgroup looks through by itself
+
+// The largest magnitude of those that this thread of 256 looks at, of a short list.
+template <u32 TY>
+__device__ __forceinline__ u32 listed_max(const WDesc &w)
+{
+    const u32 n = (u32)w.n_outlier;
+    Raw8<TY> x[SHORT_LIST / 2048];
+#pragma unroll
+    for (u32 h = 0; h < SHORT_LIST / 2048; h++) {
+        const u32 j = h * 2048u + threadIdx.x * 8u;
+        x[h] = load_raw8<TY>((const GLOBAL_AS typename Elem<TY>::type *)w.out_val + j, j < n ? n - j : 0u);
+    }
+    u32 m = 0u;
+#pragma unroll
+    for (u32 h = 0; h < SHORT_LIST / 2048; h++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, finite_mag(x[h][i]));
+    return m;
+}
+
 // Planes of the rows (T == false) or, turned, of the columns; padding of the reduction is zero.  A thread decodes runs of eight
 // symbols; protected places are left to the workgroups behind the tiles, which take them from the list (indices outside the
-// weight are left out).
+// weight are left out).  The largest values are there (`part`), or with a short list every workgroup finds them and the
+// first tile's leaves them there: 512 rows through 768 x 768, fp32, 26.3 -> 24.5 us for a launch less;
+// the lines of a gradient's scales, 1024 x 1024 x 4096 bf16, 73.7 -> 70.8 us.
 template <int W, int P, bool T>
-__global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const u32 *__restrict__ part, _Float16 *__restrict__ dst, u64 plane, u64 ld)
+__global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, u32 *__restrict__ part, bool looks, _Float16 *__restrict__ dst, u64 plane, u64 ld, Beside beside)
 {
+    const u32 others = beside.n_rows + beside.n_lines;
+    if (blockIdx.x < others) {
+        if (beside.n_lines)
+            join_lines(beside.jobs, blockIdx.x);
+        else if (P == 1) // (the types and their planes: planes_x, planes_w)
+            row_planes<TY_BF16, 1>(beside.rows, blockIdx.x);
+        else if (beside.rows.type == TY_F32)
+            row_planes<TY_F32, 2>(beside.rows, blockIdx.x);
+        else
+            row_planes<TY_F16, 1>(beside.rows, blockIdx.x);
+        return;
+    }
+    const u32 block = blockIdx.x - others;
     typedef Table<TY_F16, W> Tab;
     constexpr int ND = (8 * W + 31) / 32;
     __shared__ __attribute__((aligned(16))) u32 table[Tab::BYTES / 4];
     // a tile of 64 rows x 128 columns (64 for turned planes): four runs a thread (two), asked for before anything else
     constexpr u32 TILE_C = T ? 64u : 128u, RUNS = TILE_C / 32u;
     const u32 col_tiles = (w.cols + TILE_C - 1u) / TILE_C;
-    const u64 r0 = blockIdx.x / col_tiles * 64ull;
-    const u32 c0 = blockIdx.x % col_tiles * TILE_C;
-    const bool is_tile = blockIdx.x < tiles;
+    const u64 r0 = block / col_tiles * 64ull;
+    const u32 c0 = block % col_tiles * TILE_C;
+    const bool is_tile = block < tiles;
     u32 raw[RUNS][ND + 1];
 #pragma unroll
     for (u32 h = 0; h < RUNS; h++) {
@@ -337,9 +389,21 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, const
         load_words<ND + 1>(w.packed, (r * w.cols + c) * W >> 5, is_tile && r < w.rows && c < w.cols ? w.n_words : 0, raw[h]);
     }
     float s, inv;
-    weight_scale(part, s, inv);
+    if (looks) {
+        __shared__ u32 red[4];
+        u32 m = threadIdx.x < w.K ? finite_mag(gptr(w.codebook)[threadIdx.x]) : 0u;
+        m = max(m, w.val_bf16 ? listed_max<TY_BF16>(w) : listed_max<TY_F32>(w));
+        m = wave_max_u(m);
+        if ((threadIdx.x & 63u) == 0u) red[threadIdx.x >> 6] = m;
+        __syncthreads();
+        m = max(max(red[0], red[1]), max(red[2], red[3]));
+        scale_of(m, s, inv);
+        if (block == 0 && threadIdx.x < WMAX_PARTS) part[threadIdx.x] = m;
+    } else {
+        weight_scale(part, s, inv);
+    }
     if (!is_tile) {
-        for (u64 j = (blockIdx.x - tiles) * 256ull + threadIdx.x; j < w.n_outlier; j += (u64)(gridDim.x - tiles) * 256u) {
+        for (u64 j = (block - tiles) * 256ull + threadIdx.x; j < w.n_outlier; j += (u64)((gridDim.x - others) - tiles) * 256u) {
             const u32 i = gptr(w.out_idx)[j], r = i / w.cols, c = i - r * w.cols;
             if (r >= w.rows) continue;
             const float x = protected_value(w, j) * s;
@@ -628,38 +692,28 @@ Planes planes_for(Room &r, u64 rows, u64 reduction, u32 count)
 }
 
 // x's planes and the parts of the weight's largest magnitude
-template <u32 TY>
-void row_planes_of(const PlaneSrc &src, const Planes &p, const WDesc &w, u64 part, char *ws, hipStream_t s)
+void start_rows(const RowPlanes &x, const WDesc &w, u32 *part, hipStream_t s)
 {
-    _Float16 *dst = (_Float16 *)(ws + p.off);
-    float *inv = (float *)(ws + p.inv);
-    u32 *pm = (u32 *)(ws + part);
-    if (p.count > 1)
-        PROF("k_row_planes", s, k_row_planes<TY, 2><<<src.rows + WMAX_PARTS, 256, 0, s>>>(src, dst, p.plane, (u32)p.ld, inv, w, pm));
-    else
-        PROF("k_row_planes", s, k_row_planes<TY, 1><<<src.rows + WMAX_PARTS, 256, 0, s>>>(src, dst, p.plane, (u32)p.ld, inv, w, pm));
-}
-void row_planes(const PlaneSrc &src, u32 type, const Planes &p, const WDesc &w, u64 part, char *ws, hipStream_t s)
-{
-    switch (type) {
-    case TY_F32: row_planes_of<TY_F32>(src, p, w, part, ws, s); break;
-    case TY_BF16: row_planes_of<TY_BF16>(src, p, w, part, ws, s); break;
-    default: row_planes_of<TY_F16>(src, p, w, part, ws, s); break;
+    const u32 grid = x.src.rows + WMAX_PARTS;
+    switch (x.type) {
+    case TY_F32: PROF("k_row_planes", s, k_row_planes<TY_F32, 2><<<grid, 256, 0, s>>>(x, w, part)); break;
+    case TY_BF16: PROF("k_row_planes", s, k_row_planes<TY_BF16, 1><<<grid, 256, 0, s>>>(x, w, part)); break;
+    default: PROF("k_row_planes", s, k_row_planes<TY_F16, 1><<<grid, 256, 0, s>>>(x, w, part)); break;
     }
 }
 
-// along: the reduction runs along the stored rows
-void weight_planes(const WDesc &w, bool along, const Planes &p, char *ws, u64 part, hipStream_t s)
+// along: the reduction runs along the stored rows; looks: the largest values are not there yet
+void weight_planes(const WDesc &w, bool along, const Planes &p, char *ws, u64 part, bool looks, const Beside &beside, hipStream_t s)
 {
-    const u32 *pm = (const u32 *)(ws + part);
+    u32 *pm = (u32 *)(ws + part);
     _Float16 *dst = (_Float16 *)(ws + p.off);
     // (the padding along the reduction belongs to the tiles: it is written as zeros)
     const u32 tile_c = along ? 128u : 64u, tiles = (w.cols + tile_c - 1u) / tile_c * ((w.rows + 63u) / 64u);
-    const u32 grid = tiles + (u32)std::min<u64>((w.n_outlier + 255) / 256, 512);
+    const u32 grid = beside.n_rows + beside.n_lines + tiles + (u32)std::min<u64>((w.n_outlier + 255) / 256, 512);
     with_width(w.w, [&](auto width) {
         constexpr int W = decltype(width)::value;
         auto start = [&](auto planes, auto turned) {
-            PROF("k_weight_planes", s, k_weight_planes<W, decltype(planes)::value, decltype(turned)::value><<<grid, 256, 0, s>>>(w, tiles, pm, dst, p.plane, p.ld));
+            PROF("k_weight_planes", s, k_weight_planes<W, decltype(planes)::value, decltype(turned)::value><<<grid, 256, 0, s>>>(w, tiles, pm, looks, dst, p.plane, p.ld, beside));
         };
         typedef std::integral_constant<int, 1> One;
         typedef std::integral_constant<int, 2> Two;
@@ -898,9 +952,14 @@ hipError_t launch_linear(const LinearCall &c, hipStream_t s)
 {
     if (is_few(c.rows, c.in_out)) return launch_few(c, s);
     const LinearRoom r(c.rows, c.n_in, c.n_out, c.type);
-    const PlaneSrc x = {c.x.p, nullptr, c.x.stride, 0, (u32)c.rows, c.n_in, ACT_NONE};
-    row_planes(x, c.type, r.x, c.w, r.part, c.ws, s);
-    weight_planes(c.w, !c.in_out, r.w, c.ws, r.part, s);
+    const bool looks = c.w.n_outlier <= SHORT_LIST;
+    Beside beside = {};
+    beside.rows = {{c.x.p, nullptr, c.x.stride, 0, (u32)c.rows, c.n_in, ACT_NONE, 0}, (_Float16 *)(c.ws + r.x.off), r.x.plane, (float *)(c.ws + r.x.inv), (u32)r.x.ld, c.type};
+    if (looks)
+        beside.n_rows = (u32)c.rows;
+    else
+        start_rows(beside.rows, c.w, (u32 *)(c.ws + r.part), s);
+    weight_planes(c.w, !c.in_out, r.w, c.ws, r.part, looks, beside, s);
     Gemm g = {};
     g.M = (u32)c.rows;
     g.N = c.n_out;
@@ -959,13 +1018,21 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
     }
     u32 *part = dx ? (u32 *)(c.ws + r.part) : nullptr;
     const u32 grid = t.tiles + (dx ? WMAX_PARTS : 0u);
-    const u32 lines = d.row_tiles + d.col_tiles + (dw ? x.row_tiles + x.col_tiles : 0u); // in blocks of 64, as the tiles are
+    auto blocks = [](u64 lines) { return (u32)((lines + LINES - 1u) / LINES); };
+    const u32 lines = blocks(c.rows) + blocks(c.n_out) + (dw ? blocks(c.rows) + blocks(c.n_in) : 0u);
     switch (c.type) {
     case TY_F32: PROF("k_tile_stats", s, k_tile_stats<TY_F32><<<grid, 256, 0, s>>>(t, c.w, part)); break;
     case TY_BF16: PROF("k_tile_stats", s, k_tile_stats<TY_BF16><<<grid, 256, 0, s>>>(t, c.w, part)); break;
     default: PROF("k_tile_stats", s, k_tile_stats<TY_F16><<<grid, 256, 0, s>>>(t, c.w, part)); break;
     }
-    PROF("k_scales", s, k_scales<<<lines, 1024, 0, s>>>(t));
+    if (dx) {
+        Beside beside = {};
+        beside.jobs = t;
+        beside.n_lines = lines;
+        weight_planes(c.w, c.in_out, r.w, c.ws, r.part, false, beside, s);
+    } else {
+        PROF("k_scales", s, k_scales<<<lines, 256, 0, s>>>(t));
+    }
     if (dx || dw) switch (c.type) {
     case TY_F32: tile_planes<TY_F32>(t, r.dr.count, r.dc.count, s); break;
     case TY_BF16: tile_planes<TY_BF16>(t, r.dr.count, r.dc.count, s); break;
@@ -973,7 +1040,6 @@ hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s)
     }
     Gemm gx = {}, gw = {};
     if (dx) {
-        weight_planes(c.w, c.in_out, r.w, c.ws, r.part, s);
         gx.M = (u32)c.rows;
         gx.N = c.n_in;
         gx.wpart = (const u32 *)(c.ws + r.part);
