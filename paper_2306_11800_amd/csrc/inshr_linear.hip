@@ -24,12 +24,14 @@ constexpr u32 GROUP = 4;
 inline u64 up(u64 v, u64 to) { return (v + to - 1) / to * to; }
 
 // Planes lie in blocks of 16 rows x 32 numbers, 1024 bytes that one load of the product takes to LDS as they are: a row's
-// four pieces of eight numbers in an order of the row's own (piece c at c ^ (row / 4 % 4)), so that the 16 rows that a
-// read of LDS touches fall into different banks.  (Rows of a row-major plane gave the loads pieces of 64 bytes, at 60 % of
+// four pieces of eight numbers in an order of the row's own (piece c at c ^ turn_of(row)), so that the lanes whose reads of LDS
+// are served together meet in different banks: the 16 rows of a piece, and also rows 0-3 and 12-15 of one piece with 4-11
+// of the next (with c ^ (row / 4 % 4) every read took four cycles more, of twelve).  (Rows of a row-major plane gave the loads pieces of 64 bytes, at 60 % of
 // what a CU takes from L2 in whole lines.)  Place of number c of row r, for planes of ld numbers a row:
+__device__ __forceinline__ u32 turn_of(u32 r) { return (0u - (r >> 2)) & 3u; }
 __device__ __forceinline__ u64 plane_at(u64 r, u64 c, u64 ld)
 {
-    return ((r >> 4) * (ld / KS) + c / KS) * (16u * KS) + (r & 15u) * KS + ((c / 8u & 3u) ^ (r >> 2 & 3u)) * 8u + (c & 7u);
+    return ((r >> 4) * (ld / KS) + c / KS) * (16u * KS) + (r & 15u) * KS + ((c / 8u & 3u) ^ turn_of((u32)r)) * 8u + (c & 7u);
 }
 
 struct PlaneSrc { // a matrix of elements; act != ACT_NONE: multiplied by the slope at the values of `pre`
@@ -569,7 +571,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemms both
     struct Operands {
         h8 a[TM], b[TN];
     } even, odd;
-    const u32 r16 = lane & 15u, piece = ((lane >> 4) ^ (r16 >> 2)) * 8u;
+    const u32 r16 = lane & 15u, piece = ((lane >> 4) ^ turn_of(r16)) * 8u;
     auto read = [&](Operands &o, u32 slot) {
         const _Float16 *as = lds + slot * SLOT + (wm + r16) * KS + piece, *bs = lds + slot * SLOT + (BM + wn + r16) * KS + piece;
 #pragma unroll
