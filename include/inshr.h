@@ -413,7 +413,7 @@ typedef struct {
  * Sums are held in fp32; a result is rounded once, `pre` on its own.  The factors are fp16 numbers scaled
  * by powers of two (one per row of x, one for the weight), in two parts each for fp32 results, one and two
  * for fp16, one each for bfloat16: what that takes from a product is 2^-22, 2^-22 and 2^-11 of it, or 2^-40
- * of (largest of the row) * (largest of the weight) where that is more.  Infinities and NaN in a row of x
+ * of (largest of the row) * (largest of the weight) where that is more.  (Few rows keep more.)  Infinities and NaN in a row of x
  * make that row's results infinite or NaN.  The call returns after enqueueing, allocates nothing and may be
  * captured into a graph; overlapping calls take workspaces of their own.  workspace: device, 256-byte
  * aligned, inshr_linear_bound() bytes (NULL when that is 0).

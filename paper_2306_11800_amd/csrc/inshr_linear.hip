@@ -9,6 +9,11 @@
 //   2 passes h h + h l          for fp16 results: fp16 activations are exact in h, the weight keeps 22 bits
 //   3 passes h h + h l + l h    for fp32 results: what is left out, l l, is 2^-22 of the product
 // (three planes of bfloat16 would need six passes for fp32, and two for bfloat16 results).
+//
+// What bounds it, measured: 2048 rows through 4096 x 11008 bf16 243 us, of which the product takes 231 (0.8 PFLOP/s, the matrix
+// cores at work in 48 % of the busy cycles; its floor at the rate of the library's largest products is 133) and the
+// weight's planes 40 (34 MB of symbols to 90 MB of planes, 3.1 TB/s).  Small products and the gradients are three to six launches
+// one after the other: 512 rows through 768 x 768 fp32 24 us, the gradients of 1024 x 1024 x 4096 bf16 66, of 515 x 1000 x 1537 fp32 51.
 #include "inshr_table.h"
 
 #include <algorithm>
@@ -121,8 +126,10 @@ __global__ __launch_bounds__(256) void k_row_planes(RowPlanes j, WDesc w, u32 *_
 // the gradient below the activation, and the activations turned round
 // ------------------------------------------------------------------------------------------
 // Both are cut into tiles of 64 x 64.  k_tile_stats takes each tile's largest magnitudes per row and per column and its
-// sums per column; k_scales joins them, in a fixed order; k_tile_planes works the values out again (they come from the
-// caches, and two planes of them would be as much to write and read) and stores the planes, the turned ones through LDS.
+// sums per column; k_scales (or the launch of the weight's planes) joins them, in a fixed order; k_tile_planes works the values
+// out again (they come from the caches, and two planes of them would be as much to write and read) and stores the
+// planes, the turned ones through LDS.  Memory and the slopes bound both: 8.4 and 10 us at 1024 x 1024 x 4096 bf16 gelu_tanh
+// (19 MB read each, 19 MB of planes written; 4 us of it a launch).
 struct TileJob {
     PlaneSrc src;
     u32 col_tiles, row_tiles;
@@ -637,7 +644,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemms both
     }
 }
 
-// The sums of the splits, in their order: eight results a thread.
+// The sums of the splits, in their order: eight results a thread.  A launch and the traffic of the sums: 5 us for 9 MB.
 template <u32 TY>
 __global__ __launch_bounds__(256) void k_join(Gemms both)
 {
@@ -744,7 +751,7 @@ constexpr u32 CUS = 256;
 constexpr u32 KIND_M[3] = {256, 128, 128}, KIND_N[3] = {256, 256, 128};
 // Measured, in 0.01 us: a step of a tile on a full chip; what a workgroup takes beside its steps (the first loads, the
 // results), and a launch of k_join; and 4 bytes of fp32 sums written and read again, in 2^-20 of it
-constexpr u32 KIND_TIME[3] = {91, 52, 30}, KIND_FIXED[3] = {900, 500, 300}, JOIN_TIME = 350, SUM_TIME = 210;
+constexpr u32 KIND_TIME[3] = {91, 52, 35}, KIND_FIXED[3] = {900, 500, 300}, JOIN_TIME = 350, SUM_TIME = 210;
 
 // The time until all workgroups are done, the ones that take longer first: n0 that take t0 each and n1 that take t1.
 u64 time_of(u32 n0, u32 t0, u32 n1, u32 t1)

@@ -164,6 +164,9 @@ __device__ void sort_descending(T *v, u32 n) // n: a power of two
 // seen are not below; at least k elements of the row are not below the smallest of these (about 1.2 k for logits in no
 // particular order).  A second reading of the row picks them out and adds the others up.  Each candidate's place is the
 // number of larger ones.
+// Bound by vector instructions: 4096 rows of 32000 bf16, k = 64, 93 us (two readings of 262 MB each, 5.6 TB/s); one row of 50257 fp32
+// 14.3 us, read by one workgroup.  Keeping the row in registers for the second reading took longer (95 -> 102 us), and
+// so did a bound from a part of the row (92 -> 102).
 template <u32 TY, u32 BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restrict__ index, float *__restrict__ value, float *__restrict__ tail)
 {
@@ -341,7 +344,8 @@ __device__ __forceinline__ int first_of(const int *idx, u32 j)
     return again ? -1 : i;
 }
 
-// The first wave ends the row: 64 lanes with up to four listed entries each.
+// One reading of the row, the first wave ends it: 64 lanes with up to four listed entries each, in fp64.  4096 rows of 50257
+// bf16, 64 listed: 134 us (3.1 TB/s; an exponential and five other vector instructions a logit beside the reading).
 template <u32 TY, u32 BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restrict__ loss, double *__restrict__ saved)
 {
@@ -436,6 +440,7 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
     }
 }
 
+// A reading and a writing of the row: 4096 rows of 50257 bf16 in 165 us (5.0 TB/s, more than a plain copy of the library reaches).
 template <u32 TY, u32 BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const double *__restrict__ saved, const float *__restrict__ g, Mat grad)
 {

@@ -108,7 +108,8 @@ def test_shapes(ctx, shape, in_out, dtype):
 
 @pytest.mark.parametrize("rows,n_in,n_out,in_out", [(2100, 130, 8200, False), (2049, 200, 8000, True), (70, 4200, 4100, False),
                                                     (66, 4097, 4500, True), (260, 9000, 70, False), (4100, 66, 130, True),
-                                                    (4096, 70, 4096, False), (2048, 70, 11008, False)])
+                                                    (4096, 70, 4096, False), (2048, 70, 11008, False),
+                                                    (1024, 1024, 4096, True)])
 def test_large_shapes(ctx, rows, n_in, n_out, in_out):
     """Many tiles of each size, or few with a long reduction."""
     rng = np.random.default_rng(rows)
