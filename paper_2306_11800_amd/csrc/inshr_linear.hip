@@ -10,9 +10,9 @@
 //   3 passes h h + h l + l h    for fp32 results: what is left out, l l, is 2^-22 of the product
 // (three planes of bfloat16 would need six passes for fp32, and two for bfloat16 results).
 //
-// What bounds it, measured: 2048 rows through 4096 x 11008 bf16 243 us, of which the product takes 231 (0.8 PFLOP/s, the matrix
+// What bounds it, measured: 2048 rows through 4096 x 11008 bf16 241 us, of which the product takes 231 (0.8 PFLOP/s, the matrix
 // cores at work in 48 % of the busy cycles; its floor at the rate of the library's largest products is 133) and the
-// weight's planes 40 (34 MB of symbols to 90 MB of planes, 3.1 TB/s).  Small products and the gradients are three to six launches
+// weight's planes 38 (34 MB of symbols to 90 MB of planes, 3.3 TB/s).  Small products and the gradients are three to six launches
 // one after the other: 512 rows through 768 x 768 fp32 24 us, the gradients of 1024 x 1024 x 4096 bf16 66, of 515 x 1000 x 1537 fp32 51.
 #include "inshr_table.h"
 
@@ -309,30 +309,33 @@ __global__ __launch_bounds__(256) void k_tile_planes(TileJobs jobs)
 // ------------------------------------------------------------------------------------------
 // the weight
 // ------------------------------------------------------------------------------------------
+constexpr u32 ONE_MARK = 0xFC00FC00u; // (minus infinity twice: no entry has a high part that is infinite and one that is left over)
+
 // Eight entries of the table into the planes, the marked ones left out.
 template <int P>
-__device__ __forceinline__ void store_entries(const u32 (&e)[8][2], u32 skip, _Float16 *at, u64 plane)
+__device__ __forceinline__ void store_entries(const u32 (&e)[8][2], _Float16 *at, u64 plane)
 {
     u4_16 hi, lo;
+    u32 least = ~0u; // 0: one is marked
+#pragma unroll
+    for (int q = 0; q < 8; q++) least = min(least, e[q][0] ^ ONE_MARK);
 #pragma unroll
     for (int q = 0; q < 4; q++) {
         hi[q] = low_halves(e[2 * q][0], e[2 * q + 1][0]);
         lo[q] = high_halves(e[2 * q][0], e[2 * q + 1][0]);
     }
-    if (skip == 0u) {
+    if (least != 0u) {
         *(u4_16 *)at = hi;
         if (P > 1) *(u4_16 *)(at + plane) = lo;
     } else {
 #pragma unroll
         for (int q = 0; q < 8; q++) {
-            if (skip >> q & 1u) continue;
+            if (e[q][0] == ONE_MARK) continue;
             ((u16 *)at)[q] = (u16)(hi[q / 2] >> (16 * (q & 1)));
             if (P > 1) ((u16 *)(at + plane))[q] = (u16)(lo[q / 2] >> (16 * (q & 1)));
         }
     }
 }
-constexpr u32 ONE_MARK = 0xFC00FC00u; // (minus infinity twice: no entry has a high part that is infinite and one that is left over)
-
 // What shares the launch with the weight: rows of activations, or the lines of a gradient's scales.
 struct Beside {
     RowPlanes rows;
@@ -385,18 +388,17 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, u32 *
     constexpr int ND = (8 * W + 31) / 32;
     __shared__ __attribute__((aligned(16))) u32 table[Tab::BYTES / 4];
     // a tile of 64 rows x 128 columns (64 for turned planes): four runs a thread (two), asked for before anything else
-    constexpr u32 TILE_C = T ? 64u : 128u, RUNS = TILE_C / 32u;
+    constexpr u32 TILE_C = T ? 64u : 128u, RUNS = TILE_C / 32u, DOWN = 2048u / TILE_C; // rows from a thread's run to its next
     const u32 col_tiles = (w.cols + TILE_C - 1u) / TILE_C;
     const u64 r0 = block / col_tiles * 64ull;
     const u32 c0 = block % col_tiles * TILE_C;
     const bool is_tile = block < tiles;
+    const u32 run = threadIdx.x % (TILE_C / 8u) * 8u, down = threadIdx.x / (TILE_C / 8u), c = c0 + run;
+    const u64 bit0 = ((r0 + down) * w.cols + c) * W, next_bits = (u64)w.cols * (DOWN * W); // (of its first run)
     u32 raw[RUNS][ND + 1];
 #pragma unroll
-    for (u32 h = 0; h < RUNS; h++) {
-        const u32 i = threadIdx.x + 256u * h, c = c0 + i % (TILE_C / 8u) * 8u;
-        const u64 r = r0 + i / (TILE_C / 8u);
-        load_words<ND + 1>(w.packed, (r * w.cols + c) * W >> 5, is_tile && r < w.rows && c < w.cols ? w.n_words : 0, raw[h]);
-    }
+    for (u32 h = 0; h < RUNS; h++)
+        load_words<ND + 1>(w.packed, (bit0 + h * next_bits) >> 5, is_tile && r0 + down + h * DOWN < w.rows && c < w.cols ? w.n_words : 0, raw[h]);
     float s, inv;
     if (looks) {
         __shared__ u32 red[4];
@@ -428,44 +430,41 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, u32 *
     __syncthreads();
     const u32 mine = lane_copy<TY_F16, W>();
     __shared__ u32 turned[T ? 64 : 1][65];
+    _Float16 *const at = dst + (T ? plane_at(c0 + (threadIdx.x >> 3), r0 + (threadIdx.x & 7u) * 8u, ld) : plane_at(r0 + down, c, ld));
 #pragma unroll
     for (u32 h = 0; h < RUNS; h++) {
-        const u32 i = threadIdx.x + 256u * h, run = i % (TILE_C / 8u), c = c0 + run * 8u;
-        const u64 r = r0 + i / (TILE_C / 8u);
+        const u64 r = r0 + down + h * DOWN;
         const u32 left = r < w.rows && c < w.cols ? w.cols - c : 0u;
         u32 d[ND + 1];
-        const u32 shift = (u32)((r * w.cols + c) * W) & 31u;
+        const u32 shift = (u32)(bit0 + h * next_bits) & 31u;
 #pragma unroll
         for (int q = 0; q < ND; q++) d[q] = __builtin_amdgcn_alignbit(raw[h][q + 1], raw[h][q], shift);
         d[ND] = 0u;
         u32 e[8][2];
-        u32 at_one = 0u; // protected places
 #pragma unroll
-        for (int q = 0; q < 8; q++) {
-            look_up<TY_F16, W>((const char *)table, mine, d, q, e[q]);
-            if ((u32)q >= left) e[q][0] = 0u;
-            at_one |= (e[q][0] == ONE_MARK ? 1u : 0u) << q;
+        for (int q = 0; q < 8; q++) look_up<TY_F16, W>((const char *)table, mine, d, q, e[q]);
+        if (left < 8u) {
+#pragma unroll
+            for (u32 q = 0; q < 8u; q++)
+                if (q >= left) e[q][0] = 0u;
         }
         if (T) {
 #pragma unroll
-            for (int q = 0; q < 8; q++) turned[i / (TILE_C / 8u)][run * 8u + q] = e[q][0];
+            for (int q = 0; q < 8; q++) turned[down + h * DOWN][run + q] = e[q][0];
         } else if (r < w.rows && c < (u32)ld) {
-            store_entries<P>(e, at_one, dst + plane_at(r, c, ld), plane);
+            store_entries<P>(e, at + h * DOWN * ld, plane); // (blocks of 16 rows follow each other)
         }
     }
     if (T) {
         __syncthreads();
 #pragma unroll
         for (u32 h = 0; h < 2u; h++) {
-            const u32 i = threadIdx.x + 256u * h, c = i >> 3, r = (i & 7u) * 8u;
-            if (c0 + c >= w.cols) continue;
-            u32 e[8][2], at_one = 0u;
+            const u32 col = (threadIdx.x >> 3) + 32u * h, r = (threadIdx.x & 7u) * 8u;
+            if (c0 + col >= w.cols) continue;
+            u32 e[8][2];
 #pragma unroll
-            for (u32 q = 0; q < 8u; q++) {
-                e[q][0] = turned[r + q][c];
-                at_one |= (e[q][0] == ONE_MARK ? 1u : 0u) << q;
-            }
-            store_entries<P>(e, at_one, dst + plane_at(c0 + c, r0 + r, ld), plane);
+            for (u32 q = 0; q < 8u; q++) e[q][0] = turned[r + q][col];
+            store_entries<P>(e, at + h * 32u * ld, plane);
         }
     }
 }

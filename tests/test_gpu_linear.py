@@ -356,6 +356,32 @@ def test_streams_and_graphs(ctx):
     c2.close()
 
 
+def test_captured_beside_the_context_s_stream(ctx):
+    """Two captured graphs of calls on a context of a third stream, replayed in turn and side by side."""
+    rng = np.random.default_rng(21)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        c2 = api.Context(torch.device(DEV))
+    layer, _, x, r = case(rng, 120, 320, 200, 16, BF16, "gelu", residual=True)
+    dy, pre = rows_of(rng, 120, 200, BF16), rows_of(rng, 120, 200, BF16)
+    streams, graphs, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    for s in streams:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append([c2.linear(layer, x, r), *c2.linear_grad(layer, x, dy, pre)])
+        graphs.append(g)
+    for k in range(3):
+        for t in (x, r, dy, pre):
+            t.copy_(torch.randn_like(t))
+        want = [ctx.linear(layer, x, r), *ctx.linear_grad(layer, x, dy, pre)]
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for out in outs for a, b in zip(want, out))
+    c2.close()
+
+
 def test_refusals(ctx):
     import ctypes as C
     rng = np.random.default_rng(15)
