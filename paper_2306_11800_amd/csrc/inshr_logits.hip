@@ -320,6 +320,7 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
 static_assert(MAX_LISTED <= 256, "a thread per listed entry");
 // Saved per row: log of the student's sum, log of its part that is not listed, log of the teacher's sum, and what the
 // unlisted ones' gradient is of their share of that part: q - P_tail e^(u - log_out) = e^(u - log_out) (q_rest - P_tail).
+// The first is +inf for a row whose loss is 0 by definition, and NaN for a row with NaN or +inf.
 constexpr int SAVED = 4;
 
 // Entry j of the row's list into idx[j], -1 for an index outside the vocabulary; idx has room for MAX_LISTED and is -1
@@ -381,7 +382,8 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
     if (tid >= 64u) return;
     // the listed ones, and the teacher's, in fp64: the loss is a small difference of logarithms
     double t[4], u[4], tail = c.tail ? (double)gptr(c.tail)[r] : -INFINITY, mt = tail, ms = -INFINITY;
-    bool any = false;
+    // what there is (NaN is there too: the maxima below pass it over)
+    bool any = false, taught = tail != -INFINITY, student = false, odd = !(tail < INFINITY);
 #pragma unroll
     for (u32 q = 0; q < 4u; q++) {
         t[q] = u[q] = -INFINITY;
@@ -391,11 +393,16 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
         any = true;
         t[q] = (double)gptr(c.value)[r * c.k + tid + 64u * q] * inv_T;
         u[q] = (double)Elem<TY>::get(p[i]) * inv_T;
-        mt = t[q] != t[q] ? t[q] : fmax(mt, t[q]);
+        mt = fmax(mt, t[q]);
         ms = fmax(ms, u[q]);
+        taught = taught || t[q] != -INFINITY;
+        student = student || u[q] != -INFINITY;
+        odd = odd || !(t[q] < INFINITY) || !(u[q] < INFINITY);
     }
-    const double log_out = joined_log<WAVES>(room, inv_T);
-    any = __ballot(any) != 0;
+    const double log_out = joined_log<WAVES>(room, inv_T); // (NaN where one of them is NaN or +inf)
+    const bool untaught = __ballot(any) == 0 || __ballot(taught) == 0;
+    odd = !untaught && __ballot(odd || log_out != log_out) != 0;
+    const bool empty = untaught || (!odd && __ballot(student || log_out != -INFINITY) == 0);
     mt = wave_max(mt);
     ms = fmax(wave_max(ms), log_out);
     double st = 0.0, ss = 0.0;
@@ -409,7 +416,6 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
     ss = wave_sum(ss);
     const double log_t = mt + log(st + (tail == -INFINITY ? 0.0 : exp(tail - mt)));
     const double log_s = ms + log(ss + (log_out == -INFINITY ? 0.0 : exp(log_out - ms)));
-    const bool empty = !any || mt == -INFINITY || ms == -INFINITY;
     // sum P (e^d - 1 - d), d = log q - log P: as the listed ones and the rest add up to 1 on both sides, errors of the two
     // logarithms of sums cancel to first order
     double all = 0.0;
@@ -430,9 +436,9 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
             all += tail == -INFINITY ? exp(lq) : exp(lp) * (expm1(lq - lp) - (lq - lp));
             if (log_out != -INFINITY) over = tail == -INFINITY ? exp(lq) : lp > lq ? exp(lp) * expm1(lq - lp) : -exp(lq) * expm1(lp - lq);
         }
-        gptr(loss)[r] = empty ? 0.0f : (float)all;
+        gptr(loss)[r] = empty ? 0.0f : odd ? __uint_as_float(0x7fc00000u) : (float)all;
         if (saved) {
-            gptr(saved)[r * SAVED + 0] = empty ? INFINITY : log_s;
+            gptr(saved)[r * SAVED + 0] = empty ? INFINITY : odd ? NAN : log_s;
             gptr(saved)[r * SAVED + 1] = log_out == -INFINITY ? 0.0 : log_out;
             gptr(saved)[r * SAVED + 2] = log_t;
             gptr(saved)[r * SAVED + 3] = over;
@@ -452,7 +458,7 @@ __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const doub
     const u32 V = c.n_vocab, tid = threadIdx.x;
     const double inv_T = 1.0 / (double)c.temperature;
     const double log_s = gptr(saved)[r * SAVED + 0];
-    const bool empty = log_s == INFINITY;
+    const bool empty = log_s == INFINITY, odd = log_s != log_s;
     const double up = (g ? (double)gptr(g)[r] : 1.0) * inv_T;
     read_list(c, r, idx);
     __syncthreads();
@@ -464,11 +470,12 @@ __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const doub
         at_mine = (float)(up * (exp(u - log_s) - exp(t - gptr(saved)[r * SAVED + 2])));
     }
     __syncthreads(); // (the gradient may take the logits' place)
-    const float f = empty ? 0.0f : (float)(up * gptr(saved)[r * SAVED + 3]);
+    const float none = odd ? __uint_as_float(0x7fc00000u) : 0.0f; // of a logit that is -inf
+    const float f = empty ? 0.0f : odd ? none : (float)(up * gptr(saved)[r * SAVED + 3]);
     // e^(z / T - log_out) = 2^(z c - l), c and l in two parts each
     const double c64 = LOG2E * inv_T, l64 = empty ? 0.0 : gptr(saved)[r * SAVED + 1] * LOG2E;
     const float ch = (float)c64, cl = (float)(c64 - (double)ch), lh = (float)l64, ll = (float)(l64 - (double)lh);
-    auto slope = [&](float x) { return empty || x == -INFINITY ? 0.0f : f * pow2(fmaf(x, ch, -lh) + fmaf(x, cl, -ll)); };
+    auto slope = [&](float x) { return empty || x == -INFINITY ? none : f * pow2(fmaf(x, ch, -lh) + fmaf(x, cl, -ll)); };
     // The steps begin where the results' lines of 128 bytes begin; an element of a step is read before it is written.
     const u32 head = min((u32)((0ull - (u64)out) & 127ull) / (u32)sizeof(T), V);
     if (tid < head) out[tid] = Elem<TY>::put(slope(Elem<TY>::get(p[tid])));

@@ -1,0 +1,70 @@
+"""GPU: rows of logits at the ends of what the header allows, against plain forms in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2306_11800_amd import api
+from tests.test_gpu_logits import logits_of, teacher_list
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = api.Context(torch.device(DEV))
+    yield c
+    c.close()
+
+
+@pytest.mark.parametrize("rows,vocab,k", [(14, 700, 12), (600, 300, 3), (14, 9000, 200)])
+def test_nan_is_never_a_loss_of_zero(ctx, rows, vocab, k):
+    """Rows with NaN or +inf have loss and gradient NaN, whatever else stands in them; a row of which the teacher says
+    nothing has 0, whatever stands in it; the rows beside them do not change."""
+    rng = np.random.default_rng(vocab)
+    for dtype in (F32, BF16):
+        t = logits_of(rng, rows, vocab, F32)
+        index, value, tail = teacher_list(t, k, 1.0)
+        for with_tail in (False, True):
+            i, v, l = index.clone(), value.clone(), tail.clone()
+            z = (t + 0.1).to(dtype)
+            top = api.TopLogits(i, v, l if with_tail else None)
+            clean, saved = ctx.distill(z, top)
+            cgrad = ctx.distill_grad(z, top, saved)
+            unlisted = int(t[3].argmin())
+            z[0] = NAN                                   # what a layer makes of a row with NaN
+            z[1] = -INF
+            z[1, i[1, 0].long()] = NAN                   # nothing but NaN is there, and it is listed
+            z[2] = -INF
+            z[2, int(t[2].argmin())] = NAN               # ... not listed
+            z[3, unlisted] = NAN
+            z[3, :unlisted] = -INF                       # the masked ones too
+            z[4] = -INF
+            z[4, i[4, -1].long()] = INF
+            z[5] = INF
+            v[6] = NAN                                   # the teacher
+            v[7] = -INF
+            v[7, -1] = NAN
+            l[7] = -INF
+            v[8, 0] = INF
+            i[9], z[9] = -1, NAN                         # padding
+            v[10], l[10], z[10] = -INF, -INF, NAN        # a teacher that allows nothing
+            if with_tail:
+                v[11], l[11] = -INF, NAN
+            else:
+                v[11] = NAN
+            i[12, 1:] = -1
+            v[12, 1:] = NAN                              # values of empty places do not count
+            loss, saved = ctx.distill(z, top)
+            grad = ctx.distill_grad(z, top, saved)
+            bad, none = [0, 1, 2, 3, 4, 5, 6, 7, 8, 11], [9, 10]
+            keep = [r for r in range(rows) if r not in bad + none + [12]]
+            assert torch.isnan(loss).nonzero()[:, 0].tolist() == bad
+            assert torch.isnan(grad).all(1).nonzero()[:, 0].tolist() == bad and not bool(torch.isnan(grad[none + keep + [12]]).any())
+            assert not bool(loss[none].any()) and not bool(grad[none].any())
+            assert torch.equal(loss[keep], clean[keep]) and torch.equal(grad[keep], cgrad[keep])
+            same = z.clone()
+            again = ctx.distill_grad(same, top, saved, out=same)
+            assert torch.equal(again.isnan(), grad.isnan()) and torch.equal(again.nan_to_num(), grad.nan_to_num())
