@@ -473,8 +473,9 @@ typedef struct {
  *   loss = sum_listed P (log P - log q) + P_tail (log P_tail - log q_rest)
  * (without a tail P_tail = 0 and the last term is not there).  A row without a listed entry, whose listed
  * values and tail are all -inf, or whose logits are all -inf, has loss 0 and gradient 0.  A loss is +inf
- * where q is 0 and P is not.  NaN or +inf among a row's logits, listed values and tail makes its loss and all of
- * its gradient NaN, unless the row has no listed entry or the teacher's values and tail are all -inf.
+ * where q is 0 and P is not (a P below the range of fp64 counts as 0).  NaN or +inf among a row's logits,
+ * listed values and tail makes its loss and all of its gradient NaN, unless the row has no listed entry or
+ * the teacher's values and tail are all -inf.
  *   loss   device fp32 [rows]
  *   saved  device fp64 [rows][INSHR_DISTILL_SAVED] for inshr_distill_grad, or NULL
  * inshr_distill_grad: d loss / d logit = (q_v - P_v) / temperature for a listed v, q_v (1 - P_tail / q_rest) /

@@ -4,11 +4,11 @@ import pytest
 import torch
 
 from paper_2306_11800_amd import api
-from tests.test_gpu_logits import logits_of, teacher_list
+from tests.test_gpu_logits import check_distill, logits_of, teacher_list
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
-F32, BF16 = torch.float32, torch.bfloat16
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 INF, NAN = float("inf"), float("nan")
 
 
@@ -68,3 +68,38 @@ def test_nan_is_never_a_loss_of_zero(ctx, rows, vocab, k):
             same = z.clone()
             again = ctx.distill_grad(same, top, saved, out=same)
             assert torch.equal(again.isnan(), grad.isnan()) and torch.equal(again.nan_to_num(), grad.nan_to_num())
+
+
+def test_teachers_far_apart(ctx):
+    """P that fp64 does not hold, where q is anything: listed values and tails far below the largest, masks of the type's
+    lowest value on either side.  (A P that is 0 in 64 bits counts as 0.)"""
+    rng = np.random.default_rng(2)
+    rows, vocab, k = 12, 400, 10
+    low = torch.finfo(F32).min
+    for T in (0.5, 1.0, 4.0):
+        for dtype in (F32, BF16, F16):
+            t = logits_of(rng, rows, vocab, F32)
+            index, value, tail = teacher_list(t, k, T)
+            z = (t + 0.3 * torch.randn_like(t)).to(dtype)
+            value[0, 4:] -= 800 * T
+            value[1, 2:] -= 720 * T                       # e^d is past fp64, P e^d is not
+            value[2, 1:] = low                            # masked by the lowest value: one allowed, and what is left
+            tail[2] = low / T if T >= 1.0 else -INF
+            tail[3] = -900.0
+            tail[4] = value[4, 0] / T - 730.0
+            value[5, 3:] = torch.finfo(BF16).min
+            value[6, 1:], tail[6] = low, -INF
+            z[7, index[7, 1:].long()] = -INF              # the student masks by -inf what the teacher masks by the lowest
+            value[7, 1:], tail[7] = low, -INF
+            value[8, 1:] -= 745 * T                       # P at the end of fp64
+            value[9, ::2] += 1000 * T
+            # (where q is 0 too the plain form has no value: a P of 0 is what -inf in the list gives)
+            runs, none = [], value.clone()
+            none[7, 1:] = -INF
+            for v in (value, none):
+                top = api.TopLogits(index, v, tail, T)
+                loss, saved = ctx.distill(z, top)
+                runs.append((loss, ctx.distill_grad(z, top, saved)))
+            assert all(torch.equal(a, b) for a, b in zip(*runs))
+            check_distill(ctx, z, index, none, tail, T)
+            check_distill(ctx, z, index, none, None, T)
