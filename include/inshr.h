@@ -479,8 +479,10 @@ typedef struct {
  *   loss   device fp32 [rows]
  *   saved  device fp64 [rows][INSHR_DISTILL_SAVED] for inshr_distill_grad, or NULL
  * inshr_distill_grad: d loss / d logit = (q_v - P_v) / temperature for a listed v, q_v (1 - P_tail / q_rest) /
- * temperature for the others (which is their share of q_rest times q_rest - P_tail, and so also where q_rest vanishes), times grad_loss (device fp32 [rows], NULL: 1), into grad [rows][n_vocab] of
- * `type`, which may be the logits themselves (same address and stride).  saved is inshr_distill's for the same arguments.
+ * temperature for the others (which is their share of q_rest times q_rest - P_tail, and so also where q_rest
+ * vanishes; unlisted logits 2^53 temperatures below the listed ones have a share of 1 each for their largest),
+ * times grad_loss (device fp32 [rows], NULL: 1), into grad [rows][n_vocab] of `type`, which may be the logits
+ * themselves (same address and stride).  saved is inshr_distill's for the same arguments.
  * Both return after enqueueing, allocate nothing and may be captured. */
 #define INSHR_DISTILL_SAVED 4
 int inshr_distill(inshr_ctx *ctx, const inshr_distill_in *in, float *loss, double *saved);

@@ -95,9 +95,10 @@ __device__ __forceinline__ void put_sum(const RowSum &a, double c, double2 *room
     s = wave_sum(s);
     if ((threadIdx.x & 63u) == 0u) room[threadIdx.x >> 6] = make_double2((double)m, s);
 }
-// The logarithm of the whole sum, -inf where nothing counts; by all lanes of a wave.
+// The whole sum: the largest logit (x) and the sum of e^((logit - x) / T) (y), 0 where nothing counts, NaN where one is NaN
+// or +inf; by all lanes of a wave.
 template <int WAVES>
-__device__ __forceinline__ double joined_log(const double2 *room, double inv_T)
+__device__ __forceinline__ double2 joined_sum(const double2 *room, double inv_T)
 {
     const u32 lane = threadIdx.x & 63u;
     double2 v = make_double2(-INFINITY, 0.0);
@@ -108,9 +109,7 @@ __device__ __forceinline__ double joined_log(const double2 *room, double inv_T)
     double s = v.y > 0.0 ? v.y * exp((v.x - m) * inv_T) : v.y;
 #pragma unroll
     for (int d = 8; d; d >>= 1) s += __shfl_xor(s, d);
-    m = __shfl(m, 0);
-    s = __shfl(s, 0);
-    return s > 0.0 ? m * inv_T + log(s) : s != s ? s : -INFINITY;
+    return make_double2(__shfl(m, 0), __shfl(s, 0));
 }
 
 template <u32 TY>
@@ -309,8 +308,8 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
         put_sum(rest, LOG2E * inv_T, room);
         __syncthreads();
         if (tid >= 64u) return;
-        const double l = joined_log<WAVES>(room, inv_T);
-        if (tid == 0) gptr(tail)[r] = odd ? __uint_as_float(0x7fc00000u) : (float)l;
+        const double2 l = joined_sum<WAVES>(room, inv_T);
+        if (tid == 0) gptr(tail)[r] = odd || l.y != l.y ? __uint_as_float(0x7fc00000u) : l.y > 0.0 ? (float)(l.x * inv_T + log(l.y)) : -INFINITY;
     }
 }
 
@@ -318,10 +317,18 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
 // the loss
 // ------------------------------------------------------------------------------------------
 static_assert(MAX_LISTED <= 256, "a thread per listed entry");
-// Saved per row: log of the student's sum, log of its part that is not listed, log of the teacher's sum, and what the
-// unlisted ones' gradient is of their share of that part: q - P_tail e^(u - log_out) = e^(u - log_out) (q_rest - P_tail).
-// The first is +inf for a row whose loss is 0 by definition, and NaN for a row with NaN or +inf.
+// Logarithms of sums are held as the largest member and the logarithm of what the sum is relative to it: added up, a
+// logit / T of 2^53 takes all digits of the second (a row masked by the type's lowest value throughout).  Saved per row:
+//   0  the student's second part; +inf for a row whose loss is 0 by definition, NaN for a row with NaN or +inf
+//   1  two floats: the student's largest logit, the largest of those that are not listed (0 where there are none)
+//   2  the teacher's second part, -0.0 or less where its largest member is the tail (as they are not below 0)
+//   3  two floats: the teacher's largest member, a listed logit or the tail; and what the gradient of an unlisted logit is
+//      of e^((logit - largest) / T): q_rest - P_tail, divided by the sum of these (by 1 where q_rest is so small that fp64 has
+//      no digits of the sum in its logarithm: unlisted logits 2^53 T below the listed ones)
 constexpr int SAVED = 4;
+__device__ __forceinline__ double two_floats(float a, float b) { return __longlong_as_double((long long)((u64)__float_as_uint(a) << 32 | __float_as_uint(b))); }
+__device__ __forceinline__ float first_float(double v) { return __uint_as_float((u32)((u64)__double_as_longlong(v) >> 32)); }
+__device__ __forceinline__ float second_float(double v) { return __uint_as_float((u32)(u64)__double_as_longlong(v)); }
 
 // Entry j of the row's list into idx[j], -1 for an index outside the vocabulary; idx has room for MAX_LISTED and is -1
 // past the list.  A barrier has to follow.
@@ -353,6 +360,15 @@ __device__ __forceinline__ double divergence(double lp, double lq)
     if (d > 1.0) return exp(lq) - (p == 0.0 ? 0.0 : p * (1.0 + d));
     return p == 0.0 ? 0.0 : p * (expm1(d) - d);
 }
+
+// A listed logit of the teacher's / T and its tail, relative to the largest member of its sum.  (Of equal logits the difference
+// is 0: taken before it is divided, as the compiler may leave a product unrounded before a subtraction.)
+struct Teacher {
+    double high, tail, inv_T; // the largest listed logit, the tail
+    bool by_tail;             // the tail is the largest
+    __device__ __forceinline__ double listed(double value) const { return by_tail ? value * inv_T - tail : (value - high) * inv_T; }
+    __device__ __forceinline__ double rest() const { return by_tail ? 0.0 : tail - high * inv_T; }
+};
 
 // One reading of the row, the first wave ends it: 64 lanes with up to four listed entries each, in fp64.  4096 rows of 50257
 // bf16, 64 listed: 134 us (3.1 TB/s; an exponential and five other vector instructions a logit beside the reading).
@@ -390,7 +406,8 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
     __syncthreads();
     if (tid >= 64u) return;
     // the listed ones, and the teacher's, in fp64: the loss is a small difference of logarithms
-    double t[4], u[4], tail = c.tail ? (double)gptr(c.tail)[r] : -INFINITY, mt = tail, ms = -INFINITY;
+    double t[4], u[4], high = -INFINITY, ms = -INFINITY;
+    const double tail = c.tail ? (double)gptr(c.tail)[r] : -INFINITY;
     // what there is (NaN is there too: the maxima below pass it over)
     bool any = false, taught = tail != -INFINITY, student = false, odd = !(tail < INFINITY);
 #pragma unroll
@@ -400,31 +417,32 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
         const int i = first_of(idx, tid + 64u * q);
         if (i < 0) continue;
         any = true;
-        t[q] = (double)gptr(c.value)[r * c.k + tid + 64u * q] * inv_T;
-        u[q] = (double)Elem<TY>::get(p[i]) * inv_T;
-        mt = fmax(mt, t[q]);
+        t[q] = (double)gptr(c.value)[r * c.k + tid + 64u * q];
+        u[q] = (double)Elem<TY>::get(p[i]);
+        high = fmax(high, t[q]);
         ms = fmax(ms, u[q]);
         taught = taught || t[q] != -INFINITY;
         student = student || u[q] != -INFINITY;
         odd = odd || !(t[q] < INFINITY) || !(u[q] < INFINITY);
     }
-    const double log_out = joined_log<WAVES>(room, inv_T); // (NaN where one of them is NaN or +inf)
+    const double2 out = joined_sum<WAVES>(room, inv_T);
     const bool untaught = __ballot(any) == 0 || __ballot(taught) == 0;
-    odd = !untaught && __ballot(odd || log_out != log_out) != 0;
-    const bool empty = untaught || (!odd && __ballot(student || log_out != -INFINITY) == 0);
-    mt = wave_max(mt);
-    ms = fmax(wave_max(ms), log_out);
+    odd = !untaught && __ballot(odd || out.y != out.y) != 0;
+    const bool empty = untaught || (!odd && __ballot(student || out.y > 0.0) == 0);
+    high = wave_max(high);
+    const Teacher teacher = {high, tail, inv_T, !(tail <= high * inv_T)};
+    ms = fmax(wave_max(ms), out.x);
     double st = 0.0, ss = 0.0;
 #pragma unroll
     for (u32 q = 0; q < 4u; q++) {
         if (64u * q >= c.k) continue;
-        if (t[q] != -INFINITY) st += exp(t[q] - mt);
-        if (u[q] != -INFINITY) ss += exp(u[q] - ms);
+        if (t[q] != -INFINITY) st += exp(teacher.listed(t[q]));
+        if (u[q] != -INFINITY) ss += exp((u[q] - ms) * inv_T);
     }
     st = wave_sum(st);
     ss = wave_sum(ss);
-    const double log_t = mt + log(st + (tail == -INFINITY ? 0.0 : exp(tail - mt)));
-    const double log_s = ms + log(ss + (log_out == -INFINITY ? 0.0 : exp(log_out - ms)));
+    const double lt = log(st + (tail == -INFINITY ? 0.0 : exp(teacher.rest())));
+    const double ls = log(ss + (out.y > 0.0 ? out.y * exp((out.x - ms) * inv_T) : 0.0));
     // the sum of the divergences: as the listed ones and the rest add up to 1 on both sides, errors of the two
     // logarithms of sums cancel to first order
     double all = 0.0;
@@ -432,24 +450,28 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
     for (u32 q = 0; q < 4u; q++) {
         if (64u * q >= c.k || empty) continue;
         if (t[q] != -INFINITY)
-            all += divergence(t[q] - log_t, u[q] - log_s);
+            all += divergence(teacher.listed(t[q]) - lt, (u[q] - ms) * inv_T - ls);
         else if (u[q] != -INFINITY)
-            all += exp(u[q] - log_s);
+            all += exp((u[q] - ms) * inv_T - ls);
     }
     all = wave_sum(all);
     if (tid == 0) {
         double over = 0.0;
         if (!empty) {
-            const double lp = tail - log_t, lq = log_out - log_s;
+            const double lp = teacher.rest() - lt, one = (out.x - ms) * inv_T - ls, lq = out.y > 0.0 ? one + log(out.y) : -INFINITY;
             all += tail == -INFINITY ? exp(lq) : divergence(lp, lq);
-            if (log_out != -INFINITY) over = tail == -INFINITY ? exp(lq) : lp > lq ? exp(lp) * expm1(lq - lp) : -exp(lq) * expm1(lp - lq);
+            if (out.y > 0.0) {
+                over = tail == -INFINITY ? exp(lq) : lp > lq ? exp(lp) * expm1(lq - lp) : -exp(lq) * expm1(lp - lq);
+                over *= exp(one - lq); // (1 / out.y, or 1 where lq has no digits for it)
+            }
         }
         gptr(loss)[r] = empty ? 0.0f : odd ? __uint_as_float(0x7fc00000u) : (float)all;
         if (saved) {
-            gptr(saved)[r * SAVED + 0] = empty ? INFINITY : odd ? NAN : log_s;
-            gptr(saved)[r * SAVED + 1] = log_out == -INFINITY ? 0.0 : log_out;
-            gptr(saved)[r * SAVED + 2] = log_t;
-            gptr(saved)[r * SAVED + 3] = over;
+            GLOBAL_AS double *to = gptr(saved) + r * SAVED;
+            to[0] = empty ? INFINITY : odd ? NAN : ls;
+            to[1] = two_floats((float)ms, out.y > 0.0 ? (float)out.x : 0.0f);
+            to[2] = copysign(lt, teacher.by_tail ? -1.0 : 1.0);
+            to[3] = two_floats((float)(teacher.by_tail ? tail : high), (float)over);
         }
     }
 }
@@ -465,25 +487,34 @@ __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const doub
     GLOBAL_AS T *out = (GLOBAL_AS T *)grad.p + r * grad.stride;
     const u32 V = c.n_vocab, tid = threadIdx.x;
     const double inv_T = 1.0 / (double)c.temperature;
-    const double log_s = gptr(saved)[r * SAVED + 0];
-    const bool empty = log_s == INFINITY, odd = log_s != log_s;
+    const GLOBAL_AS double *kept = gptr(saved) + r * SAVED;
+    const double ls = kept[0], lt = kept[2];
+    const bool empty = ls == INFINITY, odd = ls != ls;
     const double up = (g ? (double)gptr(g)[r] : 1.0) * inv_T;
     read_list(c, r, idx);
     __syncthreads();
     const int mine = tid < c.k ? first_of(idx, tid) : -1;
     float at_mine = 0.0f;
     if (mine >= 0 && !empty) {
-        const double t = (double)gptr(c.value)[r * c.k + tid] * inv_T;
-        const double u = (double)Elem<TY>::get(p[mine]) * inv_T;
-        at_mine = (float)(up * (exp(u - log_s) - exp(t - gptr(saved)[r * SAVED + 2])));
+        const double most = (double)first_float(kept[3]);
+        const Teacher teacher = {most, most, inv_T, (bool)signbit(lt)};
+        const double t = teacher.listed((double)gptr(c.value)[r * c.k + tid]);
+        const double u = ((double)Elem<TY>::get(p[mine]) - (double)first_float(kept[1])) * inv_T;
+        at_mine = (float)(up * (exp(u - ls) - exp(t - fabs(lt))));
     }
     __syncthreads(); // (the gradient may take the logits' place)
-    const float none = odd ? __uint_as_float(0x7fc00000u) : 0.0f; // of a logit that is -inf
-    const float f = empty ? 0.0f : odd ? none : (float)(up * gptr(saved)[r * SAVED + 3]);
-    // e^(z / T - log_out) = 2^(z c - l), c and l in two parts each
-    const double c64 = LOG2E * inv_T, l64 = empty ? 0.0 : gptr(saved)[r * SAVED + 1] * LOG2E;
+    const float f = empty ? 0.0f : odd ? __uint_as_float(0x7fc00000u) : (float)(up * (double)second_float(kept[3]));
+    // e^((z - m) / T) = 2^((z - base) c - l), l = (m - base) c, c and l in two parts each.  No base (0) where l has few enough
+    // digits before the point: z - 0 is not rounded.  What is below `least` counts as that: its share is 0, and no term is infinite.
+    const double c64 = LOG2E * inv_T, m = empty ? 0.0 : (double)second_float(kept[1]);
+    const float base = fabs(m * c64) < 1048576.0 && c64 < 1048576.0 ? 0.0f : (float)m;
+    const double l64 = (m - (double)base) * c64;
     const float ch = (float)c64, cl = (float)(c64 - (double)ch), lh = (float)l64, ll = (float)(l64 - (double)lh);
-    auto slope = [&](float x) { return empty || x == -INFINITY ? none : f * pow2(fmaf(x, ch, -lh) + fmaf(x, cl, -ll)); };
+    const float least = -(float)fmin((300.0 + fabs(l64)) / c64, 3.4e38);
+    auto slope = [&](float x) {
+        const float d = fmaxf(x - base, least), s = f * pow2(fmaf(d, ch, -lh) + fmaf(d, cl, -ll));
+        return empty ? 0.0f : s;
+    };
     // The steps begin where the results' lines of 128 bytes begin; an element of a step is read before it is written.
     const u32 head = min((u32)((0ull - (u64)out) & 127ull) / (u32)sizeof(T), V);
     if (tid < head) out[tid] = Elem<TY>::put(slope(Elem<TY>::get(p[tid])));

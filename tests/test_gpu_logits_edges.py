@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2306_11800_amd import api
-from tests.test_gpu_logits import check_distill, logits_of, teacher_list
+from tests.test_gpu_logits import check_distill, check_top, logits_of, teacher_list
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -103,3 +103,41 @@ def test_teachers_far_apart(ctx):
             assert all(torch.equal(a, b) for a, b in zip(*runs))
             check_distill(ctx, z, index, none, tail, T)
             check_distill(ctx, z, index, none, None, T)
+
+
+def test_small_temperatures(ctx):
+    """A masked or large logit times log2 e / T leaves the range of fp32, and of two logarithms that far out nothing but the
+    difference is left.  (A tail of 13 / T has to lie within fp32.)"""
+    rng = np.random.default_rng(3)
+    rows, vocab, k = 8, 3000, 7
+    for T in (1e-3, 1e-8, 1e-12, 1e-30, 2.0 ** -120):
+        for dtype in (F32, BF16):
+            t = logits_of(rng, rows, vocab, F32)
+            t[3] = torch.finfo(F32).min
+            t[3, 5:9] = torch.tensor([1.0, 1.0, 2.0, 0.5], device=DEV)
+            t[4] *= min(T, 1.0) * 2.0                     # logits that lie T apart
+            index, value, _ = teacher_list(t, k, 1.0)
+            z = t.clamp(torch.finfo(dtype).min, -torch.finfo(dtype).min).to(dtype)
+            z[0, ::3] = torch.finfo(dtype).min
+            top = check_top(ctx, z, k, T)
+            # (loss and gradient of other rows are of the size of 1 / T, which fp32 holds down to 1e-30 or so)
+            scale = torch.full((rows,), 2.0 ** -20 * T, device=DEV)
+            check_distill(ctx, z, top.index, top.value, top.tail, T, scale)
+
+
+def test_logits_near_the_end_of_the_range(ctx):
+    rng = np.random.default_rng(4)
+    for dtype in (F32, BF16):
+        z = logits_of(rng, 7, 1000, dtype)
+        z[0, 100:110] = 3.2e38
+        z[1, 50] = -3.2e38
+        z[2] = -3.0e38
+        z[2, ::5] = -2.9e38
+        z[3, 17] = 3.2e38
+        z[4] = torch.finfo(dtype).min                 # all masked by the lowest value
+        z[5] = torch.finfo(dtype).min                 # all but one
+        z[5, 500] = 1.0
+        z[6] = 1e-30
+        index, value, tail = teacher_list(z, 30, 1.0)
+        check_distill(ctx, z, index, value, tail, 1.0)
+        check_distill(ctx, z, index, value, None, 0.7)
