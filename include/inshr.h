@@ -451,7 +451,8 @@ int inshr_linear_grad(inshr_ctx *ctx, const inshr_layer *layer, inshr_matrix x, 
  *   value  device fp32 [rows][k], the logits
  *   tail   device fp32 [rows] or NULL: log of the sum of exp(logit / temperature) over the logits that are
  *          not listed; -inf when these are all -inf or there are none, NaN for a row with NaN or +inf.
- * temperature > 0, finite.  Returns after enqueueing, allocates nothing and may be captured. */
+ * temperature >= 2^-126 (the smallest normal number), finite.  Returns after enqueueing, allocates nothing and
+ * may be captured. */
 int inshr_top_logits(inshr_ctx *ctx, inshr_matrix logits, uint32_t type, uint64_t rows, uint32_t n_vocab, uint32_t k,
                      float temperature, int32_t *index, float *value, float *tail);
 
@@ -464,7 +465,7 @@ typedef struct {
     const float *tail;    /* device [rows], or NULL: the teacher has nothing but the listed logits      */
     uint64_t rows;        /* 0 .. 2^22 */
     uint32_t n_vocab, k, type;
-    float temperature;
+    float temperature; /* >= 2^-126, finite */
 } inshr_distill_in;
 
 /* Distillation from a teacher's top logits.  Per row, with t the listed values / temperature and u the

@@ -2456,7 +2456,8 @@ int logits_of(const inshr_matrix &m, uint32_t type, uint64_t rows, uint32_t n_vo
 {
     if (type > INSHR_F16 || rows > MAX_ROWS || n_vocab == 0 || n_vocab > INSHR_MAX_VOCAB) return INSHR_E_ARG;
     if (k == 0 || k > INSHR_MAX_LISTED || k > n_vocab) return INSHR_E_ARG;
-    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return INSHR_E_ARG;
+    // (below the normal numbers log2 e / temperature is past fp32)
+    if (!(temperature >= 0x1p-126f) || !std::isfinite(temperature)) return INSHR_E_ARG;
     if (rows && !matrix_ok(m, type, n_vocab, true, false)) return INSHR_E_ARG;
     memset(&l, 0, sizeof(l));
     l.logits = mat(m);

@@ -141,3 +141,15 @@ def test_logits_near_the_end_of_the_range(ctx):
         index, value, tail = teacher_list(z, 30, 1.0)
         check_distill(ctx, z, index, value, tail, 1.0)
         check_distill(ctx, z, index, value, None, 0.7)
+
+
+def test_temperatures_below_the_normal_numbers_are_refused(ctx):
+    z = torch.zeros((4, 100), device=DEV)
+    top = ctx.top_logits(z, 5, 2.0 ** -126)
+    for T in (1e-39, 1e-45):
+        with pytest.raises(RuntimeError):
+            ctx.top_logits(z, 5, T)
+        top.temperature = T
+        with pytest.raises(RuntimeError):
+            ctx.distill(z, top)
+    ctx.sync()
