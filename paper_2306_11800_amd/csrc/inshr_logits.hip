@@ -33,15 +33,17 @@ __device__ __forceinline__ void add8(RowSum &a, const float (&v)[8], float m8, f
 #pragma unroll
     for (int i = 0; i < 8; i++) a.s += pow2((v[i] - a.m) * c);
 }
-__device__ __forceinline__ void add1(RowSum &a, float x, float c)
+// `n` more of one value
+__device__ __forceinline__ void add_equal(RowSum &a, float x, float n, float c)
 {
     if (x > a.m) {
-        a.s = a.s * pow2((a.m - x) * c) + 1.0f;
+        a.s = a.s * pow2((a.m - x) * c) + n;
         a.m = x;
     } else if (a.m != -INFINITY) {
-        a.s += pow2((x - a.m) * c);
+        a.s += n * pow2((x - a.m) * c);
     }
 }
+__device__ __forceinline__ void add1(RowSum &a, float x, float c) { add_equal(a, x, 1.0f, c); }
 
 // A row in steps of eight elements a thread: work(first element, the eight, number of them there) for all of them, four
 // steps asked for at a time.  Steps that are there for every thread are worked on without a look at the row's end.
@@ -77,6 +79,18 @@ __device__ __forceinline__ double wave_sum(double v)
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ __forceinline__ u32 wave_sum_u(u32 v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ __forceinline__ u32 wave_min_u(u32 v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = min(v, __shfl_xor(v, d));
     return v;
 }
 __device__ __forceinline__ double wave_max(double v)
@@ -126,6 +140,7 @@ constexpr int TOP_MAXIMA = 4;   // a thread keeps the largest of as many parts o
 
 __device__ __forceinline__ u32 logit_key(float x) { return x != x ? 0xFFFFFFFFu : key_of_float(x); }
 __device__ __forceinline__ float logit_of(u32 key) { return __uint_as_float(bits_of_key(key)); }
+constexpr u32 KEY_OF_NONE = 0x007FFFFFu; // of -inf: the least of all
 
 // A number that at least k of the wave's keys are not below: the k-th largest, cut to its upper 20 bits.
 __device__ __forceinline__ u32 wave_kth(const u32 (&m)[TOP_MAXIMA], u32 k)
@@ -198,8 +213,10 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
 #pragma unroll
     for (int w = 1; w < WAVES; w++) thr = min(thr, low[w]);
 
+    if (thr <= KEY_OF_NONE) thr = KEY_OF_NONE + 1u; // (all that is allowed, which may be fewer than k)
     const float bound = logit_of(thr); // (NaN where the keys that were cut off it are those of NaN)
     RowSum rest = row_sum();
+    u32 least = ~0u;  // of the candidates' keys
     bool odd = false; // NaN or +inf
     each_step<TY, BLOCK>(p, V, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
         float v[8];
@@ -211,8 +228,9 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
             for (u32 q = 0; q < 8u; q++)
                 if (!(v[q] < bound) && q < there) {
                     odd = odd || !(v[q] < INFINITY);
-                    const u32 at = atomicAdd(&n_cand, 1u);
-                    if (at < TOP_ROOM) cand[at] = (u64)logit_key(v[q]) << 32 | (u32)~(i + q);
+                    const u32 at = atomicAdd(&n_cand, 1u), key = logit_key(v[q]);
+                    if (at < TOP_ROOM) cand[at] = (u64)key << 32 | (u32)~(i + q);
+                    least = min(least, key);
                     v[q] = -INFINITY;
                 }
             m8 = largest8(v);
@@ -221,41 +239,67 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
     });
     odd = __syncthreads_or(odd ? 1 : 0) != 0;
     u32 n = n_cand;
-    if (n > TOP_ROOM) {
-        // Too many, mostly equal ones: the key of rank k, the larger ones, and the first of the equal ones.  The first
-        // try is whether fewer than k lie above the bound, as in a row with fewer than k allowed logits; then by halving.
-        u32 lo = thr, hi = 0xFFFFFFFFu; // count(>= lo) >= k
-        for (bool first = true; lo < hi; first = false) {
-            const u32 mid = first ? lo + 1u : lo + (hi - lo) / 2u + 1u;
+    if (n > TOP_ROOM || n < k) {
+        // Too few: the first of those that are not allowed.  Too many, mostly equal ones (masked by a finite value): the key of
+        // rank k, the larger ones, and the first of the equal ones.  The first try is whether fewer than k lie above the least
+        // candidate, as in such a row; then by halving.
+        u32 lo = KEY_OF_NONE;
+        if (n > TOP_ROOM) {
+            if (tid == 0) count = ~0u;
             __syncthreads();
-            if (tid == 0) count = 0u;
+            least = wave_min_u(least);
+            if ((tid & 63u) == 0u) atomicMin(&count, least);
             __syncthreads();
-            u32 have = 0u;
-            each_step<TY, BLOCK>(p, V, [&](u32, const Raw8<TY> &x, u32 there, u32) {
+            lo = count;
+            u32 hi = 0xFFFFFFFFu, there_are = n; // not below lo, at least k
+            for (bool first = true; lo < hi; first = false) {
+                const u32 mid = first ? lo + 1u : lo + (hi - lo) / 2u + 1u;
+                __syncthreads();
+                if (tid == 0) count = 0u;
+                __syncthreads();
+                u32 have = 0u;
+                each_step<TY, BLOCK>(p, V, [&](u32, const Raw8<TY> &x, u32 there, u32) {
 #pragma unroll
-                for (u32 q = 0; q < 8u; q++) have += q < there && logit_key(x[q]) >= mid ? 1u : 0u;
-            });
-            if (have) atomicAdd(&count, have);
+                    for (u32 q = 0; q < 8u; q++) have += q < there && logit_key(x[q]) >= mid ? 1u : 0u;
+                });
+                have = wave_sum_u(have);
+                if ((tid & 63u) == 0u) atomicAdd(&count, have);
+                __syncthreads();
+                if (count >= k) {
+                    lo = mid;
+                    there_are = count;
+                } else {
+                    hi = mid - 1u;
+                }
+            }
             __syncthreads();
-            if (count >= k)
-                lo = mid;
-            else
-                hi = mid - 1u;
+            if (tid == 0) n_cand = 0u;
+            __syncthreads();
+            rest = row_sum();
+            const float equal_to = logit_of(lo);
+            each_step<TY, BLOCK>(p, V, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
+                float v[8];
+#pragma unroll
+                for (u32 q = 0; q < 8u; q++) v[q] = q < there ? x[q] : -INFINITY;
+                float m8 = largest8(v);
+                if (!(m8 < equal_to)) {
+#pragma unroll
+                    for (u32 q = 0; q < 8u; q++) {
+                        const u32 key = logit_key(v[q]);
+                        if (key < lo || q >= there) continue;
+                        if (key > lo) cand[atomicAdd(&n_cand, 1u)] = (u64)key << 32 | (u32)~(i + q); // (fewer than k)
+                        v[q] = -INFINITY;
+                    }
+                    m8 = largest8(v);
+                }
+                add8(rest, v, m8, c2);
+            });
+            if (tid == 0 && there_are > k) add_equal(rest, equal_to, (float)(there_are - k), c2);
+            __syncthreads();
+            n = n_cand;
         }
-        __syncthreads();
-        if (tid == 0) n_cand = 0u;
-        __syncthreads();
-        rest = row_sum();
-        for (u32 i = tid; i < V; i += BLOCK) {
-            const float x = Elem<TY>::get(p[i]);
-            const u32 key = logit_key(x);
-            if (key > lo) cand[atomicAdd(&n_cand, 1u)] = (u64)key << 32 | (u32)~i; // (fewer than k)
-            if (key < lo) add1(rest, x, c2);
-        }
-        __syncthreads();
-        n = n_cand;
         u32 equal = 0u; // equal ones before this step of the row, the same in all threads
-        for (u32 i0 = 0; i0 < V; i0 += BLOCK) {
+        for (u32 i0 = 0; i0 < V && n + equal < k; i0 += BLOCK) {
             const u32 i = i0 + tid;
             const bool is = i < V && logit_key(Elem<TY>::get(p[i])) == lo;
             const u64 mask = __ballot(is);
@@ -267,13 +311,8 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
                 if (w < (int)(tid >> 6)) before += counts[w];
                 equal += counts[w];
             }
-            if (is) {
-                const u32 at = n + before + (u32)__popcll(mask & ((1ull << (tid & 63u)) - 1ull));
-                if (at < k)
-                    cand[at] = (u64)lo << 32 | (u32)~i;
-                else if (lo != key_of_float(-INFINITY))
-                    add1(rest, logit_of(lo), c2);
-            }
+            const u32 at = n + before + (u32)__popcll(mask & ((1ull << (tid & 63u)) - 1ull));
+            if (is && at < k) cand[at] = (u64)lo << 32 | (u32)~i;
         }
         __syncthreads();
         n = k;

@@ -153,3 +153,30 @@ def test_temperatures_below_the_normal_numbers_are_refused(ctx):
         with pytest.raises(RuntimeError):
             ctx.distill(z, top)
     ctx.sync()
+
+
+@pytest.mark.parametrize("vocab", [300, 512, 1000, 1500, 1536, 2048, 2049, 8192, 8500, 50257])
+def test_top_of_masked_rows(ctx, vocab):
+    """Most of a row masked, by -inf or by finite values, in one piece or scattered: fewer than k allowed, exactly k, and
+    more than there is room for; equal logits around the last place."""
+    rng = np.random.default_rng(vocab)
+    for rows, dtype in ((16, F32), (16, BF16), (600, BF16)):
+        z = logits_of(rng, rows, vocab, dtype)
+        some = torch.from_numpy(rng.permutation(vocab)).to(DEV)
+        for r, mask in enumerate((-INF, -1000.0, torch.finfo(dtype).min)):
+            for j, allowed in enumerate((some[:30], torch.arange(vocab - 40, vocab, device=DEV), some[:64])):
+                keep = z[4 * r + j, allowed]
+                z[4 * r + j] = mask
+                z[4 * r + j, allowed] = keep
+            z[4 * r + 3, vocab - vocab // 8:] = mask
+        z[12] = -1000.0                                   # everything equal, and ...
+        z[12, some[0]] = -2000.0
+        z[13] = (z[13] * 2).round() / 2                   # many equal ones everywhere
+        z[14] = -5.0
+        z[14, some[:vocab // 2]] = -3.0                   # half of the row is what the last places are taken from
+        z[14, some[:3]] = 1.0
+        z[15, 1:] = -INF
+        for k in (1, 30, 64, 65, 256):
+            top = check_top(ctx, z, k, 2.0)
+            again = ctx.top_logits(z, k, 2.0)
+            assert torch.equal(top.index, again.index) and torch.equal(top.tail, again.tail)
