@@ -136,7 +136,8 @@ __device__ __forceinline__ const GLOBAL_AS typename Elem<TY>::type *row_of(const
 // the largest logits
 // ------------------------------------------------------------------------------------------
 constexpr u32 TOP_ROOM = 2048; // candidates
-constexpr int TOP_MAXIMA = 4;   // a thread keeps the largest of as many parts of its elements (every fourth step)
+// a thread keeps the largest of as many parts of its elements: every fourth step, or in a row of one step two elements each
+constexpr int TOP_MAXIMA = 4;
 
 __device__ __forceinline__ u32 logit_key(float x) { return x != x ? 0xFFFFFFFFu : key_of_float(x); }
 __device__ __forceinline__ float logit_of(u32 key) { return __uint_as_float(bits_of_key(key)); }
@@ -156,8 +157,28 @@ __device__ __forceinline__ u32 wave_kth(const u32 (&m)[TOP_MAXIMA], u32 k)
     return t;
 }
 
+// The same of the workgroup's keys, for rows whose elements lie in a few waves (the others are masked, or the row is short).
+template <int WAVES>
+__device__ __forceinline__ u32 group_kth(const u32 (&m)[TOP_MAXIMA], u32 k, u32 (&counts)[2][WAVES])
+{
+    u32 t = 0u;
+    for (int b = 31; b >= 12; b--) {
+        const u32 c = t | 1u << b;
+        u32 n = 0u;
+#pragma unroll
+        for (int i = 0; i < TOP_MAXIMA; i++) n += (u32)__popcll(__ballot(m[i] >= c));
+        if ((threadIdx.x & 63u) == 0u) counts[b & 1][threadIdx.x >> 6] = n;
+        __syncthreads(); // (the step after the next writes here again, and waits for this one's readers in between)
+        n = 0u;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) n += counts[b & 1][w];
+        if (n >= k) t = c;
+    }
+    return t;
+}
+
 template <class T>
-__device__ void sort_descending(T *v, u32 n) // n: a power of two
+__device__ __forceinline__ void sort_descending(T *v, u32 n) // n: a power of two
 {
     for (u32 size = 2; size <= n; size <<= 1)
         for (u32 step = size >> 1; step; step >>= 1) {
@@ -176,7 +197,9 @@ __device__ void sort_descending(T *v, u32 n) // n: a power of two
 
 // The k largest in three steps.  Every wave finds a number that ceil(k / waves) of the largest keys its threads have
 // seen are not below; at least k elements of the row are not below the smallest of these (about 1.2 k for logits in no
-// particular order).  A second reading of the row picks them out and adds the others up.  Each candidate's place is the
+// particular order).  Where a wave has seen too few that are allowed, or its share is half of its threads in a short row, the
+// waves look for a number together, with 20 barriers (without it all of a row was candidates: 1000 rows of 1000 bf16, k = 64,
+// 33 -> 14 us, 100 rows of 8192 with the last eighth masked 82 -> 15; where it is not needed it costs 1 to 2 us).  A second reading of the row picks them out and adds the others up.  Each candidate's place is the
 // number of larger ones.
 // Bound by vector instructions: 4096 rows of 32000 bf16, k = 64, 93 us (two readings of 262 MB each, 5.6 TB/s); one row of 50257 fp32
 // 14.3 us, read by one workgroup.  Keeping the row in registers for the second reading took longer (95 -> 102 us), and
@@ -186,7 +209,7 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
 {
     constexpr int WAVES = BLOCK / 64;
     __shared__ u64 cand[TOP_ROOM];
-    __shared__ u32 low[WAVES], counts[WAVES];
+    __shared__ u32 low[WAVES], counts[2][WAVES];
     __shared__ double2 room[WAVES];
     __shared__ u32 n_cand, count;
     const u64 r = blockIdx.x;
@@ -196,16 +219,24 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
     const float c2 = (float)(LOG2E * inv_T);
 
     float high[TOP_MAXIMA] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    each_step<TY, BLOCK>(p, V, [&](u32, const Raw8<TY> &x, u32 there, u32 j) {
-        float v[8];
+    if (V <= BLOCK * 8u) {
+        const u32 left = V - min(tid * 8u, V);
+        const Raw8<TY> x = load_raw8<TY>(p + tid * 8u, left);
 #pragma unroll
-        for (u32 q = 0; q < 8u; q++) v[q] = q < there ? x[q] : -INFINITY;
-        high[j] = largest(high[j], largest8(v));
-    });
+        for (u32 q = 0; q < 8u; q++)
+            if (q < left) high[q / 2u] = largest(high[q / 2u], x[q]);
+    } else {
+        each_step<TY, BLOCK>(p, V, [&](u32, const Raw8<TY> &x, u32 there, u32 j) {
+            float v[8];
+#pragma unroll
+            for (u32 q = 0; q < 8u; q++) v[q] = q < there ? x[q] : -INFINITY;
+            high[j] = largest(high[j], largest8(v));
+        });
+    }
     u32 top[TOP_MAXIMA];
 #pragma unroll
     for (int j = 0; j < TOP_MAXIMA; j++) top[j] = logit_key(high[j]);
-    const u32 mine = wave_kth(top, (k + WAVES - 1u) / WAVES);
+    const u32 share = (k + WAVES - 1u) / WAVES, mine = wave_kth(top, share);
     if ((tid & 63u) == 0u) low[tid >> 6] = mine;
     if (tid == 0) n_cand = 0u;
     __syncthreads();
@@ -213,6 +244,7 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
 #pragma unroll
     for (int w = 1; w < WAVES; w++) thr = min(thr, low[w]);
 
+    if (thr <= KEY_OF_NONE || (share >= 32u && V <= BLOCK * 16u)) thr = group_kth<WAVES>(top, k, counts);
     if (thr <= KEY_OF_NONE) thr = KEY_OF_NONE + 1u; // (all that is allowed, which may be fewer than k)
     const float bound = logit_of(thr); // (NaN where the keys that were cut off it are those of NaN)
     RowSum rest = row_sum();
@@ -304,12 +336,12 @@ __global__ __launch_bounds__(BLOCK) void k_top_logits(LogitsCall c, int *__restr
             const bool is = i < V && logit_key(Elem<TY>::get(p[i])) == lo;
             const u64 mask = __ballot(is);
             __syncthreads();
-            if ((tid & 63u) == 0u) counts[tid >> 6] = (u32)__popcll(mask);
+            if ((tid & 63u) == 0u) counts[0][tid >> 6] = (u32)__popcll(mask);
             __syncthreads();
             u32 before = equal;
             for (int w = 0; w < WAVES; w++) {
-                if (w < (int)(tid >> 6)) before += counts[w];
-                equal += counts[w];
+                if (w < (int)(tid >> 6)) before += counts[0][w];
+                equal += counts[0][w];
             }
             const u32 at = n + before + (u32)__popcll(mask & ((1ull << (tid & 63u)) - 1ull));
             if (is && at < k) cand[at] = (u64)lo << 32 | (u32)~i;
