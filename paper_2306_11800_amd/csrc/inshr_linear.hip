@@ -609,6 +609,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void k_product(Gemms both
         step(even, odd, t);
         step(odd, even, t + 1u);
     }
+    wait_and_meet<0>(); // (the last step's loads once more are still on their way, of all waves, to where the sums go next)
     // The sums go through LDS, 32 or 64 rows of a wave at a time, so that eight lanes hold a row's 64 columns.
     constexpr int MOST = (int)(D * SLOT / (WAVES * 128)), ROWS = WM <= MOST && WM <= 64 ? WM : MOST >= 64 ? 64 : 32; // (64 floats a row)
     static_assert(WN % 64 == 0 && WM % ROWS == 0 && ROWS <= MOST, "every wave has its rows in LDS");
