@@ -410,10 +410,11 @@ typedef struct {
  *   y         [rows][n_out]
  *   pre       [rows][n_out] or NULL: receives x W^T + bias, which inshr_linear_grad wants
  * y and pre share no memory with each other, with x or (but for y as above) with the residual.
- * Sums are held in fp32; a result is rounded once, `pre` on its own.  The factors are fp16 numbers scaled
- * by powers of two (one per row of x, one for the weight), in two parts each for fp32 results, one and two
- * for fp16, one each for bfloat16: what that takes from a product is 2^-22, 2^-22 and 2^-11 of it, or 2^-40
- * of (largest of the row) * (largest of the weight) where that is more.  (Few rows keep more.)  Infinities and NaN in a row of x
+ * Sums are held in fp32; a result is rounded once, `pre` on its own.  The factors are fp16 numbers scaled by powers
+ * of two (one per row of x, one for the weight): for bfloat16 one each, for fp16 one for x and two for the weight,
+ * for fp32 two each.  That takes from a product at most 2^-11, 2^-23 and 2^-21 of it, or, where this is more, 2^-38 of
+ * (largest of the row) * (largest of the weight).  Up to 96 rows with [n_out][n_in] a bfloat16 product keeps 2^-17,
+ * and up to 4 rows with [n_in][n_out] all products are those of fp32.  Infinities and NaN in a row of x
  * make that row's results infinite or NaN.  The call returns after enqueueing, allocates nothing and may be
  * captured into a graph; overlapping calls take workspaces of their own.  workspace: device, 256-byte
  * aligned, inshr_linear_bound() bytes (NULL when that is 0).
@@ -434,6 +435,9 @@ int inshr_linear(inshr_ctx *ctx, const inshr_layer *layer, inshr_matrix x, inshr
  *   dbias  device fp32 [n_out]: the sum of d over the rows         or NULL
  * x is needed for dw, pre (as inshr_linear left it) for every activation but INSHR_ACT_NONE.  The weight
  * counts as its decoded values: dw is the gradient of each of them, pruned and protected ones included.
+ * d is worked out in fp32 and, below an activation, takes part with 11 bits for dx of bfloat16 and with two fp16
+ * numbers otherwise.  From a product that takes at most, for dx: 2^-21 in fp32, 2^-23 in fp16 (2^-21 below an
+ * activation), 2^-11 in bfloat16 (2^-10); for dw: 2^-21 in fp32, 2^-23 below an activation, nothing otherwise.
  * rows == 0 sets dw and dbias to zero.  The sums are taken in the same order in every call.  dx and dw do not share
  * memory with the inputs.  Everything else as inshr_linear; at least one result is wanted.  The bound is
  * for the results named: want_dx, want_dw. */

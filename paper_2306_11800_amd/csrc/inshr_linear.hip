@@ -5,9 +5,11 @@
 // normal fp16 number and nothing is off by more than 2^-40 of it; a second plane of fp16 numbers takes what the first one
 // leaves over (22 bits together).  With h and l for the planes of either side a product takes
 //   1 pass   h h                for bfloat16 results: a factor rounded to 11 bits is off by 2^-11 at most, an eighth of
-//                               the result's own 2^-8, and bfloat16 activations (8 bits) are exact in h
-//   2 passes h h + h l          for fp16 results: fp16 activations are exact in h, the weight keeps 22 bits
-//   3 passes h h + h l + l h    for fp32 results: what is left out, l l, is 2^-22 of the product
+//                               the result's own 2^-8 (a quarter where both are rounded, as in the gradient below an
+//                               activation), and bfloat16 activations (8 bits) are exact in h
+//   2 passes h h + h l          for fp16 results: fp16 activations are exact in h, the weight is off by 2^-23
+//   3 passes h h + h l + l h    for fp32 results: what is left out, l l, is 2^-22 of the product, and each factor off by 2^-23
+// (two passes for bfloat16 would double what bounds the large products, for a tenth of the results one step of 2^-8 nearer.)
 // (three planes of bfloat16 would need six passes for fp32, and two for bfloat16 results).
 //
 // What bounds it, measured: 2048 rows through 4096 x 11008 bf16 241 us, of which the product takes 231 (0.8 PFLOP/s, the matrix

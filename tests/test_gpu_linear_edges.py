@@ -1,0 +1,36 @@
+"""GPU: layers at the ends of what the header allows, against plain forms in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2306_11800_amd import api
+from tests import answers as A
+from tests.test_gpu_linear import case, f64, near, rows_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = api.Context(torch.device(DEV))
+    yield c
+    c.close()
+
+
+def test_bits_of_a_product(ctx):
+    """Of one product a result, what the header says: 2^-21 of it for fp32 (and the rounding of the result), with few and
+    with many rows and in the gradients; dw of exact factors is rounded once."""
+    rng = np.random.default_rng(9)
+    for rows in (3, 40, 300):
+        for in_out in (False, True):
+            layer, W, x, _ = case(rng, rows, 1, 500, 256, F32, in_out=in_out, bias=False)
+            y = f64(ctx.linear(layer, x))
+            want = f64(x) @ W.t()
+            near(y, want, (2.0 ** -21 + 2.0 ** -24) * want.abs() + 2.0 ** -38 * f64(x).abs() * W.abs().max() + A.TINY[F32])
+    for dtype, bits in ((F32, 2.0 ** -21 + 2.0 ** -24), (BF16, 2.0 ** -24), (F16, 2.0 ** -24)):
+        layer, W, x, _ = case(rng, 1, 300, 200, 16, dtype, bias=False)
+        dy = rows_of(rng, 1, 200, dtype)
+        want = f64(dy).t() @ f64(x)
+        near(ctx.linear_grad(layer, x, dy)[1], want, bits * want.abs() + A.TINY[F32])
