@@ -20,7 +20,8 @@ template <u32 TY>
 __device__ __forceinline__ void entry_of(float v, float s, u32 (&e)[2])
 {
     if (TY == TY_BF16) {
-        const u32 hi = Elem<TY_BF16>::put(v);
+        // (to nearest, but not to infinity: past the largest bfloat16 number the second part takes what is cut off)
+        const u32 m = __float_as_uint(v) & 0x7fffffffu, hi = m >= 0x7f7f8000u && m < 0x7f800000u ? bf16_cut(v) >> 16 : Elem<TY_BF16>::put(v);
         const float rest = v - __uint_as_float(hi << 16);
         e[0] = hi | (u32)Elem<TY_BF16>::put(rest) << 16;
     } else if (TY == TY_F16) {

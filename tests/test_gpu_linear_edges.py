@@ -5,7 +5,7 @@ import torch
 
 from paper_2306_11800_amd import api
 from tests import answers as A
-from tests.test_gpu_linear import case, f64, near, rows_of
+from tests.test_gpu_linear import case, check_linear, f64, near, rows_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -34,3 +34,18 @@ def test_bits_of_a_product(ctx):
         dy = rows_of(rng, 1, 200, dtype)
         want = f64(dy).t() @ f64(x)
         near(ctx.linear_grad(layer, x, dy)[1], want, bits * want.abs() + A.TINY[F32])
+
+
+def test_centres_at_the_end_of_the_range(ctx):
+    """Centres above the largest bfloat16 number, times rows that bring the products back."""
+    rng = np.random.default_rng(6)
+    for in_out in (False, True):
+        codes = A.Codes(rng, 96 * 40, 4, 0)
+        codes.centres = np.array([-3.4e38, -1.0, 3.39e38, 3.4028234e38], np.float32)
+        codes.decode()
+        layer = api.QuantizedLayer(codes.quantized(api, DEV), 40, 96, in_out)
+        W = torch.from_numpy(codes.values)
+        W = W.view(96, 40).t() if in_out else W.view(40, 96)
+        for rows in (2, 20, 120):
+            for dtype in (F32, BF16):
+                check_linear(ctx, layer, W, rows_of(rng, rows, 96, dtype) * 2.0 ** -100, None)
