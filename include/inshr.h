@@ -419,8 +419,8 @@ typedef struct {
  * captured into a graph; overlapping calls take workspaces of their own.  workspace: device, 256-byte
  * aligned, inshr_linear_bound() bytes (NULL when that is 0).
  * The codes are taken as they are (inshr_dequantize checks them): a symbol above K + 1 makes the results
- * that it enters NaN, listed indices outside the weight are left out, and with a list that is not the
- * stream's ascending one the results are undefined.
+ * that it enters NaN, listed indices outside the weight are left out, and without a list (n_outlier == 0) a protected
+ * symbol counts as 0; with a list that is not the stream's ascending one the results are undefined.
  * INSHR_E_ARG: a NULL or misaligned pointer, an unknown type or activation, dimensions out of range,
  * weight.n != n_out * n_in, an output stride below its columns, an output that begins where it may not; INSHR_E_CONFIG: the codes' bits / bins;
  * INSHR_E_CAPACITY: workspace_bytes too small. */

@@ -428,7 +428,8 @@ __global__ __launch_bounds__(256) void k_weight_planes(WDesc w, u32 tiles, u32 *
         return;
     }
     fill_table<TY_F16, W>(w, table, s);
-    if (threadIdx.x >= Tab::COPIES && threadIdx.x < 2u * Tab::COPIES) table[threadIdx.x] = ONE_MARK; // (this thread's entry)
+    // (this thread's entry; without a list nobody would write the places that are left out)
+    if (w.n_outlier && threadIdx.x >= Tab::COPIES && threadIdx.x < 2u * Tab::COPIES) table[threadIdx.x] = ONE_MARK;
     __syncthreads();
     const u32 mine = lane_copy<TY_F16, W>();
     __shared__ u32 turned[T ? 64 : 1][65];

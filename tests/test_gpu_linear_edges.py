@@ -5,7 +5,7 @@ import torch
 
 from paper_2306_11800_amd import api
 from tests import answers as A
-from tests.test_gpu_linear import case, check_linear, f64, near, rows_of
+from tests.test_gpu_linear import case, check_grad, check_linear, f64, near, rows_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -49,3 +49,25 @@ def test_centres_at_the_end_of_the_range(ctx):
         for rows in (2, 20, 120):
             for dtype in (F32, BF16):
                 check_linear(ctx, layer, W, rows_of(rng, rows, 96, dtype) * 2.0 ** -100, None)
+
+
+@pytest.mark.parametrize("in_out", [False, True], ids=["oi", "io"])
+def test_a_protected_symbol_without_a_list_counts_as_zero(ctx, in_out):
+    """... in few rows, many rows and the gradients alike."""
+    rng = np.random.default_rng(7)
+    codes = A.Codes(rng, 130 * 70, 12, 900)
+    codes.protected = codes.protected * 0.0
+    codes.decode()
+    q = codes.quantized(api, DEV)
+    q.n_outlier = 0
+    layer = api.QuantizedLayer(q, 70, 130, in_out)
+    W = torch.from_numpy(codes.values)
+    W = W.view(130, 70).t() if in_out else W.view(70, 130)
+    for dtype in (F32, BF16, F16):
+        for rows in (1, 3, 30, 200):
+            stale = torch.full((1 << 22,), float("nan"), device=DEV)  # what a workspace may hold
+            torch.cuda.synchronize()
+            del stale
+            x = rows_of(rng, rows, 130, dtype)
+            check_linear(ctx, layer, W, x, None)
+            check_grad(ctx, layer, W, x, rows_of(rng, rows, 70, dtype), None)
