@@ -438,8 +438,8 @@ int inshr_linear(inshr_ctx *ctx, const inshr_layer *layer, inshr_matrix x, inshr
  * d is worked out in fp32 and, below an activation, takes part with 11 bits for dx of bfloat16 and with two fp16
  * numbers otherwise.  From a product that takes at most, for dx: 2^-21 in fp32, 2^-23 in fp16 (2^-21 below an
  * activation), 2^-11 in bfloat16 (2^-10); for dw: 2^-21 in fp32, 2^-23 below an activation, nothing otherwise.
- * rows == 0 sets dw and dbias to zero.  The sums are taken in the same order in every call.  dx and dw do not share
- * memory with the inputs.  Everything else as inshr_linear; at least one result is wanted.  The bound is
+ * rows == 0 sets dw and dbias to zero.  The sums are taken in the same order in every call.  The results do not share
+ * memory with each other or with the inputs.  Everything else as inshr_linear; at least one result is wanted.  The bound is
  * for the results named: want_dx, want_dw. */
 int inshr_linear_grad_bound(const inshr_layer *layer, uint64_t rows, uint32_t want_dx,
                             uint32_t want_dw, uint64_t *workspace_bytes);

@@ -2557,6 +2557,7 @@ int inshr_linear_grad(inshr_ctx *c, const inshr_layer *layer, inshr_matrix x, in
     if (!aligned(dw, 4) || !aligned(dbias, 4)) return INSHR_E_ARG;
     for (const void *result : {(const void *)dx.data, (const void *)dw, (const void *)dbias})
         if (rows && result && (result == x.data || result == dy.data || result == pre.data)) return INSHR_E_ARG;
+    if ((dw && (const void *)dw == (const void *)dbias) || (rows && dx.data && (dx.data == (void *)dw || dx.data == (void *)dbias))) return INSHR_E_ARG;
     rc = workspace_ok(c, "inshr_linear_grad", workspace, workspace_bytes,
                       linear_grad_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->activation,
                                         dx.data != nullptr, dw != nullptr));

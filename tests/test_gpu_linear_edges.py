@@ -1,4 +1,6 @@
 """GPU: layers at the ends of what the header allows, against plain forms in 64 bits."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -71,3 +73,19 @@ def test_a_protected_symbol_without_a_list_counts_as_zero(ctx, in_out):
             x = rows_of(rng, rows, 130, dtype)
             check_linear(ctx, layer, W, x, None)
             check_grad(ctx, layer, W, x, rows_of(rng, rows, 70, dtype), None)
+
+
+def test_results_in_one_place_are_refused(ctx):
+    rng = np.random.default_rng(8)
+    layer, _, x, _ = case(rng, 4, 64, 64, 16, F32)
+    dy, room = rows_of(rng, 4, 64, F32), torch.empty((64, 64), device=DEV)
+    c, need = layer._c[0], C.c_uint64()
+    assert ctx.lib.inshr_linear_grad_bound(C.byref(c), 4, 1, 1, C.byref(need)) == 0
+    ws = torch.empty(need.value, dtype=torch.uint8, device=DEV)
+    m = lambda t: api.CMatrix(t.data_ptr(), 64)  # noqa: E731
+    grad = lambda dx, dw, db: ctx.lib.inshr_linear_grad(  # noqa: E731
+        ctx.h, C.byref(c), m(x), m(dy), api.CMatrix(None, 0), dx, dw, db, 4, ws.data_ptr(), need.value)
+    p, none = room.data_ptr(), api.CMatrix(None, 0)
+    assert grad(m(room), p, None) == -1 and grad(m(room), None, p) == -1 and grad(none, p, p) == -1
+    assert grad(m(room), torch.empty(64 * 64, device=DEV).data_ptr(), None) == 0
+    ctx.sync()
