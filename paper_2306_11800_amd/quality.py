@@ -69,6 +69,8 @@ def weight_gradients(ctx: api.Context, steps: Sequence[Step], x: torch.Tensor, k
     that was quantized."""
     top = ctx.top_logits(teacher_logits(steps, x), k, temperature)
     h, pre = student_states(ctx, steps, x, for_gradients=True)
+    if x.dtype == torch.float16:  # (a share of the mean over many rows is less than the smallest number of this type, 6e-8)
+        h, pre = [t.float() for t in h], [t if t is None else t.float() for t in pre]
     _, saved = ctx.distill(h[-1], top)
     each = torch.full((x.shape[0],), 1.0 / x.shape[0], dtype=torch.float32, device=x.device)
     d: List[Optional[torch.Tensor]] = [None] * len(h)
