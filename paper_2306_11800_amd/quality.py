@@ -72,7 +72,7 @@ def weight_gradients(ctx: api.Context, steps: Sequence[Step], x: torch.Tensor, k
     if x.dtype == torch.float16:  # (a share of the mean over many rows is less than the smallest number of this type, 6e-8)
         h, pre = [t.float() for t in h], [t if t is None else t.float() for t in pre]
     _, saved = ctx.distill(h[-1], top)
-    each = torch.full((x.shape[0],), 1.0 / x.shape[0], dtype=torch.float32, device=x.device)
+    each = torch.full((x.shape[0],), 1.0 / max(1, x.shape[0]), dtype=torch.float32, device=x.device)
     d: List[Optional[torch.Tensor]] = [None] * len(h)
     d[-1] = ctx.distill_grad(h[-1], top, saved, each)
     out: List[torch.Tensor] = [None] * len(steps)  # type: ignore[list-item]

@@ -47,3 +47,10 @@ def test_gradients_from_fp16_states(ctx):
         for j, g in ((i, below @ W), (s.residual, into[i + 1])):
             if j is not None:
                 into[j] = g if into[j] is None else into[j] + g
+
+
+def test_no_rows(ctx):
+    rng = np.random.default_rng(2)
+    steps, _, _ = chain(ctx, rng, 4)
+    for g, s in zip(quality.weight_gradients(ctx, steps, torch.empty((0, 48), device=DEV)), steps):
+        assert g.numel() == s.layer.n_in * s.layer.n_out and not bool(g.any())
