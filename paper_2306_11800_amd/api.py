@@ -979,7 +979,8 @@ class Context:
     def _enter(self, *used):
         """Where torch works on another stream than the context's: the context's waits for it and it for the context's
         afterwards, the tensors (and layers) in use are kept from being reused too early, and what is allocated
-        meanwhile belongs to the context's stream."""
+        meanwhile belongs to the context's stream.  So a graph of calls can be captured on any stream, but not of a context
+        of the default stream."""
         return _NO_TURN if _current_stream(self._device.index) == self._stream_ptr else _Turn(self.stream, used)
 
     def _rows_of(self, t: torch.Tensor, cols: int, name: str):
@@ -1127,6 +1128,8 @@ class _Turn:
     """A call on the context's stream between what torch's current stream has done and will do."""
 
     def __init__(self, stream, used):
+        if stream.cuda_stream == 0 and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the context works on the default stream, which cannot be captured: make one on another stream")
         self.stream, self.tensors = stream, []
         for t in used:
             if isinstance(t, QuantizedLayer):

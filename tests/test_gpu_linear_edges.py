@@ -89,3 +89,28 @@ def test_results_in_one_place_are_refused(ctx):
     assert grad(m(room), p, None) == -1 and grad(m(room), None, p) == -1 and grad(none, p, p) == -1
     assert grad(m(room), torch.empty(64 * 64, device=DEV).data_ptr(), None) == 0
     ctx.sync()
+
+
+def test_a_context_of_the_default_stream_is_not_captured(ctx):
+    """... but refuses, and leaves the capture as it was."""
+    rng = np.random.default_rng(10)
+    layer, _, x, _ = case(rng, 20, 64, 40, 16, F32)
+    dy = rows_of(rng, 20, 40, F32)
+    assert ctx.stream.cuda_stream == 0
+    want, top = ctx.linear(layer, x), ctx.top_logits(x, 4)
+    _, saved = ctx.distill(x, top)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        twice = x * 2.0
+        for call in (lambda: ctx.linear(layer, x), lambda: ctx.linear_grad(layer, x, dy), lambda: ctx.top_logits(x, 4),
+                     lambda: ctx.distill(x, top), lambda: ctx.distill_grad(x, top, saved)):
+            with pytest.raises(RuntimeError, match="default stream"):
+                call()
+        again = twice + x
+    for _ in range(3):
+        x.copy_(torch.randn_like(x))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(twice, x * 2.0) and torch.equal(again, x * 2.0 + x)
+    assert ctx.linear(layer, x).shape == want.shape
