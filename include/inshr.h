@@ -559,7 +559,7 @@ int inshr_neighbourhood_search(const inshr_score *scores, const uint32_t *cell_c
                                uint32_t *best_cell, uint32_t *feasible, uint32_t *trials);
 
 /* Per-kernel timing for benchmarks (not part of the method): when enabled, every kernel launch of
- * this process is bracketed by HIP events on its stream.  inshr_profile(ctx, 1) clears the totals
+ * this process is bracketed by HIP events on its stream (but for launches into a capture, which run later).  inshr_profile(ctx, 1) clears the totals
  * and starts recording, inshr_profile(ctx, 0) stops.  inshr_profile_read synchronises the stream
  * and returns the accumulated time and launch count per kernel name (*n = number of names; at most
  * cap entries are written to out, which may be NULL to query the count). */

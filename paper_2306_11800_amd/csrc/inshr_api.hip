@@ -89,7 +89,7 @@ struct inshr_ctx {
 // ------------------------------------------------------------------------------------------
 namespace {
 struct ProfState {
-    bool on = false;
+    bool on = false, open = false;      // (open: between the two events of a launch)
     std::vector<hipEvent_t> pool;       // event pairs, reused
     std::vector<const char *> pending;  // name of each recorded pair
     std::vector<std::string> names;
@@ -101,7 +101,11 @@ struct ProfState {
 namespace inshr {
 void prof_begin(const char *name, hipStream_t s)
 {
+    g_prof.open = false;
     if (!g_prof.on) return;
+    // (a launch that is captured does not run now, and an event recorded there has no time)
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) return;
     const size_t k = g_prof.pending.size();
     while (g_prof.pool.size() < 2 * (k + 1)) {
         hipEvent_t e;
@@ -110,10 +114,12 @@ void prof_begin(const char *name, hipStream_t s)
     }
     g_prof.pending.push_back(name);
     (void)hipEventRecord(g_prof.pool[2 * k], s);
+    g_prof.open = true;
 }
 void prof_end(hipStream_t s)
 {
-    if (!g_prof.on || g_prof.pending.empty()) return;
+    if (!g_prof.open) return;
+    g_prof.open = false;
     const size_t k = g_prof.pending.size() - 1;
     (void)hipEventRecord(g_prof.pool[2 * k + 1], s);
 }

@@ -114,3 +114,31 @@ def test_a_context_of_the_default_stream_is_not_captured(ctx):
         torch.cuda.synchronize()
         assert torch.equal(twice, x * 2.0) and torch.equal(again, x * 2.0 + x)
     assert ctx.linear(layer, x).shape == want.shape
+
+
+def test_captured_while_profiled(ctx):
+    """A launch that is captured is not timed, and the calls after it go on."""
+    rng = np.random.default_rng(11)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        c2 = api.Context(torch.device(DEV))
+    layer, _, x, _ = case(rng, 120, 64, 40, 16, F32)
+    want = ctx.linear(layer, x)
+    torch.cuda.synchronize()
+    c2.profile(True)
+    try:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            y = c2.linear(layer, x)
+        assert c2.profile_read() == {}
+        for _ in range(3):
+            y.zero_()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(y, want) and torch.equal(c2.linear(layer, x), want)
+        times = c2.profile_read()
+        assert times["k_product"][1] == 3 and all(n == 3 and ms > 0 for ms, n in times.values())
+    finally:
+        c2.profile(False)
+    c2.close()
