@@ -142,3 +142,75 @@ def test_captured_while_profiled(ctx):
     finally:
         c2.profile(False)
     c2.close()
+
+
+class Bytes:
+    """A weight of n values made on the device: 128 centres, so that a symbol is a byte."""
+
+    def __init__(self, n, protected, seed):
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.sym = torch.randint(0, 129, (-(-n // 8) * 8,), generator=gen, device=DEV, dtype=torch.uint8)
+        self.sym += self.sym >= 1
+        self.sym[n:] = 0
+        index = torch.cat([torch.randint(0, n, (protected,), generator=gen, device=DEV), torch.tensor([0, n - 1], device=DEV)]).unique()
+        self.sym[index] = 1
+        centres = torch.zeros(256, device=DEV)
+        centres[:128] = torch.randn(128, generator=gen, device=DEV).mul_(0.05).sort().values
+        value = torch.randn(index.numel(), generator=gen, device=DEV).sign() * 0.2
+        self.n, self.index, self.value = n, index, value.double()
+        self.table = torch.cat([torch.zeros(2, device=DEV), centres[:128]]).double()
+        self.q = api.Quantized(n, 0, (self.sym.view(torch.int64), centres, centres, index.to(torch.int32), value), bins=128)
+        self.q.n_outlier = index.numel()
+
+    def at(self, places):
+        """The values of these places (a tensor of any shape), in 64 bits."""
+        v = self.table[self.sym[places].long()]
+        j = torch.searchsorted(self.index, places).clamp_max(self.index.numel() - 1)
+        return torch.where(self.index[j] == places, self.value[j], v)
+
+
+def check_columns(ctx, w, layer, x, cols, dy=None):
+    """The outputs `cols` of linear, and (for dy) the inputs `cols` of its gradient."""
+    n_in, n_out = layer.n_in, layer.n_out
+    if dy is None:
+        got, rows_, K = ctx.linear(layer, x)[:, cols], x.double(), n_in
+        r, c = cols[:, None], torch.arange(n_in, device=DEV)[None, :]
+    else:
+        got, rows_, K = ctx.linear_grad(layer, x, dy, want_dw=False, want_dbias=False)[0][:, cols], dy.double(), n_out
+        r, c = torch.arange(n_out, device=DEV)[None, :], cols[:, None]
+    W = w.at(c * n_out + r if layer.in_out else r * n_in + c)
+    want, S = (rows_ @ W.t()).cpu(), (rows_.abs() @ W.abs().t()).cpu()
+    top = rows_.abs().amax(1, keepdim=True).cpu() * 0.25
+    near(got, want, A.tol_sum(S, K, x.dtype, top) * (1 + A.HALF[x.dtype]) + A.HALF[x.dtype] * want.abs() + A.TINY[x.dtype])
+
+
+@pytest.mark.parametrize("in_out", [False, True], ids=["oi", "io"])
+def test_streams_of_more_than_2_32_bits(ctx, in_out):
+    n_out, n_in = (8200, 65539) if in_out else (65539, 8200)
+    w = Bytes(n_in * n_out, 4000, 3)
+    assert w.n * 8 > 1 << 32
+    layer = api.QuantizedLayer(w.q, n_out, n_in, in_out)
+    rng = np.random.default_rng(1)
+    cols = lambda n: torch.cat([torch.arange(40), torch.from_numpy(rng.integers(0, n, 40)), torch.arange(n - 40, n)]).to(DEV)  # noqa: E731
+    for rows, dtype in ((1, BF16), (3, F32), (30, F16), (130, BF16)):
+        check_columns(ctx, w, layer, rows_of(rng, rows, n_in, dtype), cols(n_out))
+    check_columns(ctx, w, layer, rows_of(rng, 70, n_in, BF16), cols(n_in), rows_of(rng, 70, n_out, BF16))
+
+
+@pytest.mark.parametrize("rows", [1, 24, 256])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_head_over_a_vocabulary(ctx, rows, dtype):
+    n_in, n_out = 1024, 50257
+    w = Bytes(n_in * n_out, 50_000, 5)
+    layer = api.QuantizedLayer(w.q, n_out, n_in)
+    rng = np.random.default_rng(rows)
+    x = rows_of(rng, rows, n_in, dtype)
+    check_columns(ctx, w, layer, x, torch.arange(n_out, device=DEV))
+    dy = rows_of(rng, rows, n_out, dtype, scale=0.01)
+    check_columns(ctx, w, layer, x, torch.arange(n_in, device=DEV), dy)
+    _, dw, db = ctx.linear_grad(layer, x, dy, want_dx=False)
+    d = dy.double()
+    want, S = (d.t() @ x.double()).cpu(), (d.abs().t() @ x.double().abs()).cpu()
+    top = (d.abs().amax(0)[:, None] * x.double().abs().amax(0)[None, :]).cpu()
+    near(dw, want, A.tol_sum(S, rows, F32, top) + 2.0 ** -24 * want.abs() + A.TINY[F32])
+    near(db, d.sum(0).cpu(), d.abs().sum(0).cpu() * rows * 2.0 ** -24 + A.TINY[F32])
