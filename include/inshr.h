@@ -387,7 +387,7 @@ int inshr_search_sketch_grid(inshr_ctx *ctx, const inshr_tensor *tensors, const 
 
 typedef struct {
     inshr_dequant_in weight; /* as inshr_quantize left it; weight.n == n_out * n_in                   */
-    uint32_t n_out, n_in;    /* 1 <= n_out, n_in <= 2^30                                               */
+    uint32_t n_out, n_in;    /* 1 <= n_out, n_in <= 2^27                                               */
     uint32_t in_out;         /* 0: the weight is stored [n_out][n_in]; nonzero: [n_in][n_out]          */
     uint32_t type;           /* INSHR_F32 ...: elements of all activations of a call                   */
     uint32_t activation;     /* INSHR_ACT_NONE ...                                                     */

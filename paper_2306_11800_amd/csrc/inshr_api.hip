@@ -2389,7 +2389,7 @@ int inshr_reconstruct(inshr_ctx *c, const inshr_codes *prev, const inshr_delta_o
 // ------------------------------------------------------------------------------------------
 namespace {
 
-constexpr uint64_t MAX_ROWS = 1ull << 22, MAX_DIM = 1ull << 30;
+constexpr uint64_t MAX_ROWS = 1ull << 22, MAX_DIM = 1ull << 27; // (beyond it a launch would have 2^32 threads, which the runtime refuses)
 
 struct OnDevice { // the context's device for the length of a call
     int before = -1;
