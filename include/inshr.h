@@ -413,7 +413,8 @@ typedef struct {
  * Sums are held in fp32; a result is rounded once, `pre` on its own.  The factors are fp16 numbers scaled by powers
  * of two (one per row of x, one for the weight): for bfloat16 one each, for fp16 one for x and two for the weight,
  * for fp32 two each.  That takes from a product at most 2^-11, 2^-23 and 2^-21 of it, or, where this is more, 2^-38 of
- * (largest of the row) * (largest of the weight).  Up to 96 rows with [n_out][n_in] a bfloat16 product keeps 2^-17,
+ * (largest of the row) * (largest of the weight).  Up to 32 rows with [n_out][n_in] (64 or 96 where a layer has
+ * few outputs) a bfloat16 product keeps 2^-17,
  * and up to 4 rows with [n_in][n_out] all products are those of fp32.  Infinities and NaN in a row of x
  * make that row's results infinite or NaN.  The call returns after enqueueing, allocates nothing and may be
  * captured into a graph; overlapping calls take workspaces of their own.  workspace: device, 256-byte

@@ -42,13 +42,24 @@ struct LinearGradCall {
     u32 n_in, n_out, in_out, type, act;
     char *ws;                // workspace, linear_grad_space() bytes
 };
-u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, bool listed);
+u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 w, bool listed); // (w: bits of a symbol)
 u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw);
 hipError_t launch_linear(const LinearCall &c, hipStream_t s);
-// Few rows: straight from the stream.  (96 rows through 4096 x 11008 take about 65 us that way and 80 by planes, 128 take 88
-// and 83.  Weights stored [in][out] have no such way for more than 4 rows.)
+// Few rows: straight from the stream.  Every block of 32 rows decodes the weight once more, which takes longer for wide symbols
+// and for fp32 (three parts, six products) and, of two weights of one size, for the one with more outputs; planes are decoded
+// once, and multiplied in two passes for fp16 and three for fp32.  Straight / by planes in us:
+//   96 rows  2048 x 2048 fp32 23/31, 4096 x 4096 bf16 of 5 bits 33/35, of 8 bits 50/38, fp32 72/48, 11008 x 4096 fp16 56/87,
+//            8192 x 8192 fp16 85/148, 1024 x 11008 bf16 40/32
+//   64 rows  8192 x 8192 fp32 98/157, 4096 x 11008 bf16 of 5 bits 53/59, of 8 bits 71/65, fp16 54/84, fp32 109/94,
+//            1024 x 50257 bf16 86/61
+//   32 rows  1024 x 50257 bf16 52/60, fp32 71/100, 256 x 30000 bf16 26/24
+// Weights stored [in][out] have no such way for more than 4 rows (4096 x 11008 bf16: 4 rows 60, 5 by planes 67).
 constexpr u32 FEW_ROWS = 96, FEW_SPLIT = 4;
-inline bool is_few(u64 rows, bool in_out) { return rows <= (in_out ? FEW_SPLIT : FEW_ROWS); }
+inline bool is_few(u64 rows, u32 n_out, bool in_out, u32 type, u32 w)
+{
+    const u32 most = type == TY_F32 || w > 7u ? 2048u : type == TY_BF16 ? 4096u : 8192u; // outputs for three blocks
+    return rows <= (in_out ? FEW_SPLIT : n_out <= most ? FEW_ROWS : n_out <= 4u * most ? 64u : 32u);
+}
 u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed);
 hipError_t launch_few(const LinearCall &c, hipStream_t s);
 hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s);

@@ -2495,7 +2495,7 @@ int inshr_linear_bound(const inshr_layer *layer, uint64_t rows, uint64_t *worksp
     WDesc w;
     const int rc = layer_of(layer, rows, w);
     if (rc) return rc;
-    *workspace_bytes = linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->weight.n_outlier != 0);
+    *workspace_bytes = linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, w.w, layer->weight.n_outlier != 0);
     return INSHR_OK;
 }
 
@@ -2515,7 +2515,7 @@ int inshr_linear(inshr_ctx *c, const inshr_layer *layer, inshr_matrix x, inshr_m
     if (y.data == x.data || y.data == pre.data) return INSHR_E_ARG;
     if (pre.data && (pre.data == x.data || pre.data == residual.data)) return INSHR_E_ARG;
     rc = workspace_ok(c, "inshr_linear", workspace, workspace_bytes,
-                      linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, layer->weight.n_outlier != 0));
+                      linear_space(rows, layer->n_in, layer->n_out, layer->in_out, layer->type, call.w.w, layer->weight.n_outlier != 0));
     if (rc) return rc;
     call.bias = layer->bias;
     call.x = mat(x);

@@ -951,9 +951,9 @@ void tile_planes(const TileJobs &t, u32 dr, u32 dc, hipStream_t s)
 
 } // namespace
 
-u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, bool listed)
+u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 w, bool listed)
 {
-    return is_few(rows, in_out) ? few_space(rows, n_in, n_out, in_out, type, listed) : LinearRoom(rows, n_in, n_out, type).bytes;
+    return is_few(rows, n_out, in_out, type, w) ? few_space(rows, n_in, n_out, in_out, type, listed) : LinearRoom(rows, n_in, n_out, type).bytes;
 }
 u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw)
 {
@@ -962,7 +962,7 @@ u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 a
 
 hipError_t launch_linear(const LinearCall &c, hipStream_t s)
 {
-    if (is_few(c.rows, c.in_out)) return launch_few(c, s);
+    if (is_few(c.rows, c.n_out, c.in_out, c.type, c.w.w)) return launch_few(c, s);
     const LinearRoom r(c.rows, c.n_in, c.n_out, c.type);
     const bool looks = c.w.n_outlier <= SHORT_LIST;
     Beside beside = {};

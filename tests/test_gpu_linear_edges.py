@@ -214,3 +214,16 @@ def test_head_over_a_vocabulary(ctx, rows, dtype):
     top = (d.abs().amax(0)[:, None] * x.double().abs().amax(0)[None, :]).cpu()
     near(dw, want, A.tol_sum(S, rows, F32, top) + 2.0 ** -24 * want.abs() + A.TINY[F32])
     near(db, d.sum(0).cpu(), d.abs().sum(0).cpu() * rows * 2.0 ** -24 + A.TINY[F32])
+
+
+@pytest.mark.parametrize("n_out", [2048, 2049, 4096, 4097, 8192, 8193, 16384, 16385])
+@pytest.mark.parametrize("dtype,bins", [(F32, 16), (BF16, 64), (BF16, 128), (F16, 16)], ids=["f32", "bf16-7", "bf16-8", "f16"])
+def test_numbers_of_rows_and_outputs(ctx, n_out, dtype, bins):
+    """Either side of the numbers at which rows go straight from the stream or by planes."""
+    rng = np.random.default_rng(n_out)
+    n_in = 70
+    codes = A.Codes(rng, n_in * n_out, bins, n_out // 4)
+    layer = api.QuantizedLayer(codes.quantized(api, DEV), n_out, n_in, activation="relu")
+    W = torch.from_numpy(codes.values).view(n_out, n_in)
+    for rows in (32, 33, 64, 65, 96, 97):
+        check_linear(ctx, layer, W, rows_of(rng, rows, n_in, dtype), rows_of(rng, rows, n_out, dtype))
