@@ -60,7 +60,7 @@ inline bool is_few(u64 rows, u32 n_out, bool in_out, u32 type, u32 w)
     const u32 most = type == TY_F32 || w > 7u ? 2048u : type == TY_BF16 ? 4096u : 8192u; // outputs for three blocks
     return rows <= (in_out ? FEW_SPLIT : n_out <= most ? FEW_ROWS : n_out <= 4u * most ? 64u : 32u);
 }
-u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed);
+u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, u32 w, bool listed);
 hipError_t launch_few(const LinearCall &c, hipStream_t s);
 hipError_t launch_linear_grad(const LinearGradCall &c, hipStream_t s);
 

@@ -389,10 +389,15 @@ __global__ __launch_bounds__(1024) void k_few_rows(Few f)
 // ------------------------------------------------------------------------------------------
 // weight [n_in][n_out]
 // ------------------------------------------------------------------------------------------
-// Consecutive outputs of a thread, 256 of which walk down the rows together.  (Runs of 16 take 4 loads where two of 8 take
-// 6, but make half the workgroups: one token through 1024 x 4096 13.1 us with 16 and 11.8 with 8, through 4096 x 11008 29.8
-// and 35.6.  Four rows' sums of 16 outputs do not fit into the registers.)
-inline u32 split_run(u32 rows, u32 n_in, u32 n_out) { return rows == 1u && (u64)n_in * n_out >= (16ull << 20) ? 16u : 8u; }
+// Consecutive outputs of a thread, 256 of which walk down the rows together.  Runs of 16 take 4 loads where two of 8 take
+// 6, but make half the workgroups, and wide symbols take more registers.  One token, runs of 8 / of 16, in us: 2048 x 4096 of 7
+// bits 15.9/17.6; 4096 x 4096 of 6 bits 19.1/21.8, of 7 bits 19.0/27.7; 4096 x 8192 of 5 bits 24.0/23.5, of 7 bits 23.4/31.6;
+// 4096 x 11008 of 6 bits 33.2/28.4, of 7 bits 32.9/39.2; 1024 x 50257 of 7 bits 52.4/42.8; 8192 x 8192 of 6 bits 35.5/29.8, of 7
+// bits 35.0/43.1.  (Four rows' sums of 16 outputs do not fit into the registers.)
+inline u32 split_run(u32 rows, u32 n_in, u32 n_out, u32 w)
+{
+    return rows == 1u && (u64)n_in * n_out >= ((w <= 6u ? 40ull : 48ull) << 20) ? 16u : 8u;
+}
 constexpr u32 SPLIT_DEPTH = 64;  // most rows of the weight that it walks down
 
 // Rows blockIdx.x % splits * depth .. of the weight.  Table: the values themselves.  Four waves walk down the rows; the
@@ -547,7 +552,7 @@ struct FewRoom {
     u64 packed = 0, turned = 0, partial = 0; // bytes (the last, or the others)
     u32 tiles = 0, steps = 0;                // of `packed`
     u32 splits = 1, depth = 1;
-    FewRoom(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed)
+    FewRoom(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, u32 w, bool listed)
     {
         if (!in_out) {
             steps = (n_in + 127u) / 128u;
@@ -558,7 +563,7 @@ struct FewRoom {
             return;
         }
         // about 768 workgroups (three a CU) where the weight has 4 rows for each at least, SPLIT_DEPTH at most
-        const u32 cols = 256u * split_run((u32)rows, n_in, n_out), blocks = (n_out + cols - 1u) / cols;
+        const u32 cols = 256u * split_run((u32)rows, n_in, n_out, w), blocks = (n_out + cols - 1u) / cols;
         depth = (u32)(((u64)n_in * blocks + 767u) / 768u);
         depth = depth < 4u ? 4u : depth > SPLIT_DEPTH ? SPLIT_DEPTH : depth;
         splits = (n_in + depth - 1u) / depth;
@@ -581,7 +586,7 @@ void start_rows(Few &f, hipStream_t s)
 template <u32 TY>
 void start_few(Few &f, const LinearCall &c, hipStream_t s)
 {
-    const FewRoom r(c.rows, c.n_in, c.n_out, c.in_out != 0, c.type, c.w.n_outlier != 0);
+    const FewRoom r(c.rows, c.n_in, c.n_out, c.in_out != 0, c.type, c.w.w, c.w.n_outlier != 0);
     if (!c.in_out) {
         f.steps = r.steps;
         f.row_blocks = f.rows <= 16u ? 1u : (f.rows + 31u) / 32u;
@@ -607,7 +612,7 @@ void start_few(Few &f, const LinearCall &c, hipStream_t s)
     f.splits = r.splits;
     f.depth = r.depth;
     f.n8 = (f.n_out + 7u) / 8u * 8u;
-    const u32 run = split_run(f.rows, f.n_in, f.n_out), grid = r.splits * ((f.n_out + 256u * run - 1u) / (256u * run));
+    const u32 run = split_run(f.rows, f.n_in, f.n_out, f.w.w), grid = r.splits * ((f.n_out + 256u * run - 1u) / (256u * run));
     with_width(f.w.w, [&](auto w) {
         constexpr int W = decltype(w)::value;
         if (f.rows > 1u)
@@ -622,9 +627,9 @@ void start_few(Few &f, const LinearCall &c, hipStream_t s)
 
 } // namespace
 
-u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, bool listed)
+u64 few_space(u64 rows, u32 n_in, u32 n_out, bool in_out, u32 type, u32 w, bool listed)
 {
-    const FewRoom r(rows, n_in, n_out, in_out, type, listed);
+    const FewRoom r(rows, n_in, n_out, in_out, type, w, listed);
     return rows ? r.packed + r.turned + r.partial : 0;
 }
 

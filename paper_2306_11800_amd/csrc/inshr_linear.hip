@@ -953,7 +953,7 @@ void tile_planes(const TileJobs &t, u32 dr, u32 dc, hipStream_t s)
 
 u64 linear_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 w, bool listed)
 {
-    return is_few(rows, n_out, in_out, type, w) ? few_space(rows, n_in, n_out, in_out, type, listed) : LinearRoom(rows, n_in, n_out, type).bytes;
+    return is_few(rows, n_out, in_out, type, w) ? few_space(rows, n_in, n_out, in_out, type, w, listed) : LinearRoom(rows, n_in, n_out, type).bytes;
 }
 u64 linear_grad_space(u64 rows, u32 n_in, u32 n_out, u32 in_out, u32 type, u32 act, bool dx, bool dw)
 {

@@ -9,8 +9,8 @@ from tests.test_answer_refusals import layer
 
 @pytest.mark.parametrize("in_out", [0, 1])
 def test_dimensions(in_out):
-    """Up to 24 threads of a launch fall to an output (96 rows, three blocks of 128 threads for 16 outputs) or to an input
-    (packing and turning 96 rows): 2^27 of either stay below the 2^32 threads that a launch may have."""
+    """Up to 16 threads of a launch fall to an output (joining the parts of 4 rows) and up to 24 to an input (packing and
+    turning 96 rows): 2^27 of either stay below the 2^32 threads that a launch may have."""
     lib, need = api.load_library(), C.c_uint64()
     for n_out, n_in, rc in ((1 << 27, 31, 0), (31, 1 << 27, 0), ((1 << 27) + 1, 4, -1), (4, (1 << 27) + 1, -1), (1 << 30, 3, -1),
                             (3, 1 << 30, -1)):

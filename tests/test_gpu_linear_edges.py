@@ -227,3 +227,13 @@ def test_numbers_of_rows_and_outputs(ctx, n_out, dtype, bins):
     W = torch.from_numpy(codes.values).view(n_out, n_in)
     for rows in (32, 33, 64, 65, 96, 97):
         check_linear(ctx, layer, W, rows_of(rng, rows, n_in, dtype), rows_of(rng, rows, n_out, dtype))
+
+
+@pytest.mark.parametrize("n_in,n_out", [(640, 65536), (640, 65544), (768, 65536), (768, 65400), (4001, 12001)])
+def test_runs_of_a_token(ctx, n_in, n_out):
+    """Weights stored [in][out] either side of the sizes at which a thread takes longer runs."""
+    w = Bytes(n_in * n_out, 20_000, n_in)
+    layer = api.QuantizedLayer(w.q, n_out, n_in, in_out=True)
+    rng = np.random.default_rng(n_out)
+    for rows, dtype in ((1, BF16), (1, F32), (2, F32)):
+        check_columns(ctx, w, layer, rows_of(rng, rows, n_in, dtype), torch.arange(n_out, device=DEV))
