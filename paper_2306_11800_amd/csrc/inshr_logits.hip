@@ -605,8 +605,12 @@ __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const doub
 namespace {
 
 // A workgroup per row: 256 threads where the rows fill the chip (eight workgroups a CU), 1024 where there are few, each of
-// which is then read in fewer steps.
-constexpr u64 FEW_LOGIT_ROWS = 512;
+// which is then read in fewer steps.  256 threads / 1024, in us:
+//   k_top_logits, one workgroup of 1024 a CU, two of which would take turns   256 rows of 50257 bf16 22.5/19.8, fp32 26.8/25.9, of
+//       131072 bf16 38/30; 384 rows of 20000 fp32 16.6/24.8, of 50257 bf16 26.8/33.0
+//   loss and gradient, two a CU   384 rows of 50257 bf16 37.1/34.5, fp32 48.5/50.4, of 131072 bf16 68/62; 768 rows of 50257 bf16
+//       50.6/54.2, of 20000 fp32 41.8/52.3
+constexpr u64 FEW_TOP_ROWS = 257, FEW_LOGIT_ROWS = 512;
 
 template <u32 TY, u32 BLOCK>
 void start_top(const LogitsCall &c, int *index, float *value, float *tail, hipStream_t s)
@@ -629,7 +633,7 @@ void start_grad(const LogitsCall &c, const double *saved, const float *g, const 
 hipError_t launch_top_logits(const LogitsCall &c, int *index, float *value, float *tail, hipStream_t s)
 {
     // (k of 1024 threads' maxima: every wave has to have seen k / 16 elements' worth of them)
-    const bool few = c.rows < FEW_LOGIT_ROWS && c.n_vocab >= 8192u;
+    const bool few = c.rows < FEW_TOP_ROWS && c.n_vocab >= 8192u;
     switch (c.type) {
     case TY_F32: few ? start_top<TY_F32, 1024>(c, index, value, tail, s) : start_top<TY_F32, 256>(c, index, value, tail, s); break;
     case TY_BF16: few ? start_top<TY_BF16, 1024>(c, index, value, tail, s) : start_top<TY_BF16, 256>(c, index, value, tail, s); break;

@@ -180,3 +180,17 @@ def test_top_of_masked_rows(ctx, vocab):
             top = check_top(ctx, z, k, 2.0)
             again = ctx.top_logits(z, k, 2.0)
             assert torch.equal(top.index, again.index) and torch.equal(top.tail, again.tail)
+
+
+def test_numbers_of_rows(ctx):
+    """Either side of the numbers of rows, and sizes of a vocabulary, at which a row has more threads."""
+    rng = np.random.default_rng(11)
+    for vocab in (8191, 8192):
+        z = logits_of(rng, 512, vocab, BF16)
+        for rows in (256, 257):
+            check_top(ctx, z[:rows], 20)
+    t = logits_of(rng, 512, 900, F32)
+    index, value, tail = teacher_list(t, 10, 1.0)
+    z = (t + 0.3 * torch.randn_like(t)).to(BF16)
+    for rows in (511, 512):
+        check_distill(ctx, z[:rows], index[:rows], value[:rows], tail[:rows], 1.0)
