@@ -237,3 +237,107 @@ def test_runs_of_a_token(ctx, n_in, n_out):
     rng = np.random.default_rng(n_out)
     for rows, dtype in ((1, BF16), (1, F32), (2, F32)):
         check_columns(ctx, w, layer, rows_of(rng, rows, n_in, dtype), torch.arange(n_out, device=DEV))
+
+
+@pytest.mark.parametrize("in_out", [False, True], ids=["oi", "io"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(130, 1, 1), (130, 300, 1), (97, 1, 300), (5, 1, 40), (3, 500, 1), (40, 2, 1),
+                                             (2, 300_007, 17), (100, 17, 100_003), (70, 100_003, 9)])
+def test_thin_layers(ctx, rows, n_in, n_out, in_out):
+    rng = np.random.default_rng(n_in + n_out)
+    for dtype in (F32, BF16):
+        layer, W, x, r = case(rng, rows, n_in, n_out, 16, dtype, "silu", in_out, residual=True)
+        check_linear(ctx, layer, W, x, r)
+        check_grad(ctx, layer, W, x, rows_of(rng, rows, n_out, dtype), rows_of(rng, rows, n_out, dtype))
+
+
+def test_rows_far_apart(ctx):
+    """Rows 2^31 elements apart, of inputs and of results: offsets of more than 32 bits."""
+    rng = np.random.default_rng(12)
+    far, rows = 1 << 31, 4
+    room = torch.empty(far * (rows - 1) + 4096, dtype=BF16, device=DEV)
+    at = lambda k, cols: room[k:].as_strided((rows, cols), (far, 1))  # noqa: E731
+    for in_out in (False, True):
+        layer, W, x, r = case(rng, rows, 200, 120, 16, BF16, "gelu", in_out, residual=True)
+        dy, pre = rows_of(rng, rows, 120, BF16), rows_of(rng, rows, 120, BF16)
+        places = [at(0, 200), at(256, 120), at(512, 120), at(768, 120)]
+        for place, t in zip(places, (x, r, dy, pre)):
+            place.copy_(t)
+        out = at(1024, 120)
+        assert torch.equal(ctx.linear(layer, places[0], places[1], out=out), ctx.linear(layer, x, r))
+        for got, want in zip(ctx.linear_grad(layer, places[0], *places[2:]), ctx.linear_grad(layer, x, dy, pre)):
+            assert torch.equal(got, want)
+    wide = A.Codes(rng, 64 * 48, 16)
+    layer = api.QuantizedLayer(wide.quantized(api, DEV), 48, 64)
+    x = rows_of(rng, 130, 64, BF16)
+    far = 1 << 25  # 130 rows by planes, the last of them past 2^32
+    place = room[:far * 129 + 64].as_strided((130, 64), (far, 1))
+    place.copy_(x)
+    assert torch.equal(ctx.linear(layer, place), ctx.linear(layer, x))
+
+
+def test_many_rows(ctx):
+    """As many rows as a call takes, through a small layer, and one more."""
+    rng = np.random.default_rng(13)
+    rows = 1 << 22
+    for dtype in (BF16, F32):
+        codes = A.Codes(rng, 12 * 9, 8, 5)
+        layer = api.QuantizedLayer(codes.quantized(api, DEV), 9, 12, activation="relu")
+        W = torch.from_numpy(codes.values).view(9, 12).to(DEV)
+        x = torch.randn((rows, 12), device=DEV).to(dtype)
+        y, pre = ctx.linear(layer, x, want_pre=True)
+        want, S = x.double() @ W.t(), x.double().abs() @ W.abs().t()
+        tol = A.tol_sum(S, 12, dtype, x.double().abs().amax(1, keepdim=True) * W.abs().max())
+        near(pre, want.cpu(), (tol * (1 + A.HALF[dtype]) + A.HALF[dtype] * want.abs() + A.TINY[dtype]).cpu())
+        assert torch.equal(y, pre.clamp_min(0.0))
+        dy = torch.randn((rows, 9), device=DEV).to(dtype)
+        dx, dw, db = ctx.linear_grad(layer, x, dy, pre)
+        d = dy.double() * (pre > 0)
+        want, S = d @ W, d.abs() @ W.abs()
+        tol = A.tol_sum(S, 9, dtype, d.abs().amax(1, keepdim=True) * W.abs().max())
+        near(dx, want.cpu(), (tol * (1 + A.HALF[dtype]) + A.HALF[dtype] * want.abs() + A.TINY[dtype]).cpu())
+        want, S = d.t() @ x.double(), d.abs().t() @ x.double().abs()
+        near(dw, want.cpu(), A.tol_sum(S, rows, F32, d.abs().amax(0)[:, None] * x.double().abs().amax(0)[None]).cpu())
+        near(db, d.sum(0).cpu(), (d.abs().sum(0) * rows * 2.0 ** -24).cpu())
+        with pytest.raises(RuntimeError):
+            ctx.linear(layer, x[:1].expand(rows + 1, 12))
+
+
+def test_non_finite_gradients(ctx):
+    """NaN and infinities in a row of dy, pre or x reach the results that they enter and no others."""
+    rng = np.random.default_rng(14)
+    for rows in (40, 200):
+        for dtype in (F32, BF16, F16):
+            for in_out in (False, True):
+                layer, _, x, _ = case(rng, rows, 96, 70, 16, dtype, "silu", in_out)
+                dy, pre = rows_of(rng, rows, 70, dtype), rows_of(rng, rows, 70, dtype)
+                dx, dw, db = ctx.linear_grad(layer, x, dy, pre)
+                dy[3, 5], pre[7, 9], x[11, 13] = float("inf"), float("nan"), float("-inf")
+                dx2, dw2, db2 = ctx.linear_grad(layer, x, dy, pre)
+                dw, dw2 = (t.t() if in_out else t for t in (dw, dw2))
+                r = [i for i in range(rows) if i not in (3, 7)]
+                o, i = [n for n in range(70) if n not in (5, 9)], [k for k in range(96) if k != 13]
+                assert torch.equal(dx[r], dx2[r]) and not bool(torch.isfinite(dx2[[3, 7]]).any())
+                assert torch.equal(db[o], db2[o]) and not bool(torch.isfinite(db2[[5, 9]]).any())
+                assert torch.equal(dw[o][:, i], dw2[o][:, i])
+                assert not bool(torch.isfinite(dw2[[5, 9]]).any()) and not bool(torch.isfinite(dw2[:, 13]).any())
+
+
+@pytest.mark.parametrize("in_out", [False, True], ids=["oi", "io"])
+def test_nothing_left(ctx, in_out):
+    """A weight whose values are all pruned, centres of zero, rows of zeros: zeros come out, and the bias."""
+    rng = np.random.default_rng(15)
+    for kind in ("pruned", "centres", "rows"):
+        codes = A.Codes(rng, 96 * 40, 8, 0, pruned=2.0 if kind == "pruned" else 0.1)
+        if kind == "centres":
+            codes.centres[:] = 0.0
+            codes.decode()
+        b = torch.randn(40, device=DEV)
+        layer = api.QuantizedLayer(codes.quantized(api, DEV), 40, 96, in_out, b)
+        for rows in (1, 3, 30, 120):
+            for dtype in (F32, BF16, F16):
+                x = rows_of(rng, rows, 96, dtype)
+                x = x * 0.0 if kind == "rows" else x
+                assert torch.equal(ctx.linear(layer, x), b.to(dtype).expand(rows, 40))
+                dx, dw, _ = ctx.linear_grad(layer, x, rows_of(rng, rows, 40, dtype))
+                assert kind == "rows" or not bool(dx.any())
+                assert kind != "rows" or not bool(dw.any())

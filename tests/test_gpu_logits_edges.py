@@ -194,3 +194,41 @@ def test_numbers_of_rows(ctx):
     z = (t + 0.3 * torch.randn_like(t)).to(BF16)
     for rows in (511, 512):
         check_distill(ctx, z[:rows], index[:rows], value[:rows], tail[:rows], 1.0)
+
+
+def test_many_rows(ctx):
+    """As many rows as a call takes, of a small vocabulary, and one more."""
+    rows = 1 << 22
+    z = torch.randn((rows, 5), device=DEV).to(BF16)
+    top = ctx.top_logits(z, 2)
+    order = z.float().sort(dim=1, descending=True, stable=True)
+    assert torch.equal(top.index.long(), order.indices[:, :2]) and torch.equal(top.value, order.values[:, :2])
+    assert float((top.tail - torch.logsumexp(order.values[:, 2:], 1)).abs().max()) < 2.0 ** -19
+    s = torch.randn((rows, 5), device=DEV).to(BF16)
+    loss, saved = ctx.distill(s, top)
+    grad = ctx.distill_grad(s, top, saved)
+    some = torch.tensor([0, 1, 65535, 65536, (1 << 21) + 3, rows - 1], device=DEV)
+    few = api.TopLogits(top.index[some], top.value[some], top.tail[some])
+    l2, s2 = ctx.distill(s[some], few)
+    assert torch.equal(loss[some], l2) or float((loss[some] - l2).abs().max()) < 2.0 ** -19
+    assert float((grad[some].float() - ctx.distill_grad(s[some], few, s2).float()).abs().max()) <= 2.0 ** -8
+    assert bool((loss >= 0).all()) and float(grad.float().sum(1).abs().max()) < 2.0 ** -6  # (five roundings of 2^-9 and less)
+    with pytest.raises(RuntimeError):
+        ctx.top_logits(z[:1].expand(rows + 1, 5), 2)
+
+
+def test_rows_far_apart(ctx):
+    """Rows 2^31 elements apart: offsets of more than 32 bits."""
+    rng = np.random.default_rng(12)
+    far, rows, vocab = 1 << 31, 4, 5000
+    room = torch.empty(far * (rows - 1) + 16384, dtype=BF16, device=DEV)
+    z, out = (room[k:].as_strided((rows, vocab), (far, 1)) for k in (1, 6000))
+    near = logits_of(rng, rows, vocab, BF16)
+    z.copy_(near)
+    a, b = ctx.top_logits(z, 30), ctx.top_logits(near, 30)
+    assert torch.equal(a.index, b.index) and torch.equal(a.value, b.value) and torch.equal(a.tail, b.tail)
+    student = (near.float() + 0.2).to(BF16)
+    z.copy_(student)
+    (la, sa), (lb, sb) = ctx.distill(z, a), ctx.distill(student, b)
+    assert torch.equal(la, lb)
+    assert torch.equal(ctx.distill_grad(z, a, sa, out=out), ctx.distill_grad(student, b, sb))
