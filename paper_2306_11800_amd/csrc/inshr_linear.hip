@@ -2,7 +2,7 @@
 //
 // Numbers: the matrix cores multiply fp16 numbers (11 bits) exactly into fp32 sums.  A row of an operand is scaled by a
 // power of two that brings its largest magnitude into [2^14, 2^15), so that everything above 2^-29 of that magnitude is a
-// normal fp16 number and nothing is off by more than 2^-40 of it; a second plane of fp16 numbers takes what the first one
+// normal fp16 number and nothing is off by more than 2^-39 of it; a second plane of fp16 numbers takes what the first one
 // leaves over (22 bits together).  With h and l for the planes of either side a product takes
 //   1 pass   h h                for bfloat16 results: a factor rounded to 11 bits is off by 2^-11 at most, an eighth of
 //                               the result's own 2^-8 (a quarter where both are rounded, as in the gradient below an
@@ -12,7 +12,7 @@
 // (two passes for bfloat16 would double what bounds the large products, for a tenth of the results one step of 2^-8 nearer.)
 // (three planes of bfloat16 would need six passes for fp32, and two for bfloat16 results).
 //
-// What bounds it, measured: 2048 rows through 4096 x 11008 bf16 241 us, of which the product takes 231 (0.8 PFLOP/s, the matrix
+// What bounds it, measured: 2048 rows through 4096 x 11008 bf16 226 to 251 us from card to card, of which the product takes 224 to 231 (0.8 PFLOP/s, the matrix
 // cores at work in 48 % of the busy cycles; its floor at the rate of the library's largest products is 133) and the
 // weight's planes 38 (34 MB of symbols to 90 MB of planes, 3.3 TB/s).  Small products and the gradients are three to six launches
 // one after the other: 512 rows through 768 x 768 fp32 24 us, the gradients of 1024 x 1024 x 4096 bf16 66, of 515 x 1000 x 1537 fp32 51.

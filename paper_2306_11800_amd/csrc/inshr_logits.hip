@@ -442,7 +442,8 @@ struct Teacher {
 };
 
 // One reading of the row, the first wave ends it: 64 lanes with up to four listed entries each, in fp64.  4096 rows of 50257
-// bf16, 64 listed: 134 us (3.1 TB/s; an exponential and five other vector instructions a logit beside the reading).
+// bf16, 64 listed: 135 us behind a gradient that has written 412 MB (3.1 TB/s; an exponential and five other vector instructions
+// a logit beside the reading), 86 when the same rows have just been read (the last-level cache has part of them).
 template <u32 TY, u32 BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restrict__ loss, double *__restrict__ saved)
 {
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(BLOCK) void k_distill(LogitsCall c, float *__restri
     }
 }
 
-// A reading and a writing of the row: 4096 rows of 50257 bf16 in 165 us (5.0 TB/s, more than a plain copy of the library reaches).
+// A reading and a writing of the row: 4096 rows of 50257 bf16 in 167 us (4.9 TB/s, more than a plain copy of the library reaches).
 template <u32 TY, u32 BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const double *__restrict__ saved, const float *__restrict__ g, Mat grad)
 {
