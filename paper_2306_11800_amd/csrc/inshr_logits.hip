@@ -575,27 +575,37 @@ __global__ __launch_bounds__(BLOCK) void k_distill_grad(LogitsCall c, const doub
         at_mine = (float)(up * (exp(u - ls) - exp(t - fabs(lt))));
     }
     __syncthreads(); // (the gradient may take the logits' place)
-    const float f = empty ? 0.0f : odd ? __uint_as_float(0x7fc00000u) : (float)(up * (double)second_float(kept[3]));
-    // e^((z - m) / T) = 2^((z - base) c - l), l = (m - base) c, c and l in two parts each.  No base (0) where l has few enough
-    // digits before the point: z - 0 is not rounded.  What is below `least` counts as that: its share is 0, and no term is infinite.
-    const double c64 = LOG2E * inv_T, m = empty ? 0.0 : (double)second_float(kept[1]);
-    const float base = fabs(m * c64) < 1048576.0 && c64 < 1048576.0 ? 0.0f : (float)m;
-    const double l64 = (m - (double)base) * c64;
-    const float ch = (float)c64, cl = (float)(c64 - (double)ch), lh = (float)l64, ll = (float)(l64 - (double)lh);
-    const float least = -(float)fmin((300.0 + fabs(l64)) / c64, 3.4e38);
-    auto slope = [&](float x) {
-        const float d = fmaxf(x - base, least), s = f * pow2(fmaf(d, ch, -lh) + fmaf(d, cl, -ll));
-        return empty ? 0.0f : s;
-    };
+    const float none = odd ? __uint_as_float(0x7fc00000u) : 0.0f; // of a logit that is -inf
+    const float f = empty || odd ? none : (float)(up * (double)second_float(kept[3]));
+    const double c64 = LOG2E * inv_T, m = empty ? 0.0 : (double)second_float(kept[1]), l64 = m * c64;
+    const float ch = (float)c64, cl = (float)(c64 - (double)ch);
     // The steps begin where the results' lines of 128 bytes begin; an element of a step is read before it is written.
-    const u32 head = min((u32)((0ull - (u64)out) & 127ull) / (u32)sizeof(T), V);
-    if (tid < head) out[tid] = Elem<TY>::put(slope(Elem<TY>::get(p[tid])));
-    each_step<TY, BLOCK>(p + head, V - head, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
-        float v[8];
+    auto row = [&](auto share) {
+        auto slope = [&](float x) {
+            const float s = f * share(x);
+            return empty || x == -INFINITY ? none : s;
+        };
+        const u32 head = min((u32)((0ull - (u64)out) & 127ull) / (u32)sizeof(T), V);
+        if (tid < head) out[tid] = Elem<TY>::put(slope(Elem<TY>::get(p[tid])));
+        each_step<TY, BLOCK>(p + head, V - head, [&](u32 i, const Raw8<TY> &x, u32 there, u32) {
+            float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; q++) v[q] = slope(x[q]);
-        store8<TY>(out + head + i, there, v);
-    });
+            for (int q = 0; q < 8; q++) v[q] = slope(x[q]);
+            store8<TY>(out + head + i, there, v);
+        });
+    };
+    // e^((z - m) / T) = 2^(z c - l), l = m c, c and l in two parts each; where l has too many digits before the point, or z c may leave
+    // fp32, 2^((z - m) c), with z - m rounded, and what is less than 2^-300 taken for that, so that no term is infinite
+    if (fabs(l64) < 1048576.0 && c64 < 1048576.0) {
+        const float lh = (float)l64, ll = (float)(l64 - (double)lh);
+        row([&](float x) { return pow2(fmaf(x, ch, -lh) + fmaf(x, cl, -ll)); });
+    } else {
+        const float mf = (float)m, least = -(float)fmin(300.0 / c64, 3.4e38);
+        row([&](float x) {
+            const float d = fmaxf(x - mf, least);
+            return pow2(fmaf(d, ch, d * cl));
+        });
+    }
     __syncthreads();
     if (mine >= 0) out[mine] = Elem<TY>::put(at_mine);
 }

@@ -232,3 +232,18 @@ def test_rows_far_apart(ctx):
     (la, sa), (lb, sb) = ctx.distill(z, a), ctx.distill(student, b)
     assert torch.equal(la, lb)
     assert torch.equal(ctx.distill_grad(z, a, sa, out=out), ctx.distill_grad(student, b, sb))
+
+
+def test_large_temperatures(ctx):
+    """Up to the largest number: every allowed logit counts the same, and what is masked by -inf counts nothing."""
+    rng = np.random.default_rng(13)
+    for T in (1e30, 3e37, 3e38):
+        for dtype in (F32, BF16):
+            t = logits_of(rng, 6, 2000, F32)
+            t[1, 1000:] = -INF
+            t[2, 4:] = -INF
+            index, value, tail = teacher_list(t, 9, T)
+            z = t.to(dtype)
+            z[3, ::2] = -INF
+            check_top(ctx, z, 9, T)
+            check_distill(ctx, z, index, value, tail, T, torch.full((6,), T / 4, device=DEV))
