@@ -414,9 +414,8 @@ typedef struct {
  * of two (one per row of x, one for the weight): for bfloat16 one each, for fp16 one for x and two for the weight,
  * for fp32 two each.  That takes from a product at most 2^-11, 2^-23 and 2^-21 of it, or, where this is more, 2^-38 of
  * (largest of the row) * (largest of the weight).  Up to 32 rows with [n_out][n_in] (64 or 96 where a layer has
- * few outputs) a bfloat16 product keeps 2^-17,
- * and up to 4 rows with [n_in][n_out] all products are those of fp32.  Infinities and NaN in a row of x
- * make that row's results infinite or NaN.  The call returns after enqueueing, allocates nothing and may be
+ * few outputs) it takes 2^-17 at most from a bfloat16 product, and up to 4 rows with [n_in][n_out] all products are
+ * those of fp32.  Infinities and NaN in a row of x make that row's results infinite or NaN.  The call returns after enqueueing, allocates nothing and may be
  * captured into a graph; overlapping calls take workspaces of their own.  workspace: device, 256-byte
  * aligned, inshr_linear_bound() bytes (NULL when that is 0).
  * The codes are taken as they are (inshr_dequantize checks them): a symbol above K + 1 makes the results
@@ -560,8 +559,8 @@ int inshr_neighbourhood_search(const inshr_score *scores, const uint32_t *cell_c
                                uint32_t *best_cell, uint32_t *feasible, uint32_t *trials);
 
 /* Per-kernel timing for benchmarks (not part of the method): when enabled, every kernel launch of
- * this process is bracketed by HIP events on its stream (but for launches into a capture, which run later).  inshr_profile(ctx, 1) clears the totals
- * and starts recording, inshr_profile(ctx, 0) stops.  inshr_profile_read synchronises the stream
+ * this process is bracketed by HIP events on its stream (but for launches into a capture, which run later).
+ * inshr_profile(ctx, 1) clears the totals and starts recording, inshr_profile(ctx, 0) stops.  inshr_profile_read synchronises the stream
  * and returns the accumulated time and launch count per kernel name (*n = number of names; at most
  * cap entries are written to out, which may be NULL to query the count). */
 typedef struct {
